@@ -427,6 +427,85 @@ us_status us_attention_bwd(const void* Q, const void* K, const void* V, const vo
 us_status us_sum_fwd(const void* X, void* Y, long rows, long n, float alpha, void* stream);
 us_status us_sum_bwd(const void* G, void* dX, long rows, long n, float beta, void* stream);
 
+/*
+ * Gated feed-forward block (SwiGLU and its relatives: gate f = silu, gelu, relu or sigmoid) as one call per direction, with the fixed factors
+ * of Table A.2 for its products and, by the rule of Sec. 5.2, alpha = 1 / rms f(z) and beta = 1 / rms f'(z), z ~ N(0,1), for the gate
+ * (us_gate_scales): the gated product f(z) u has the second moment of f(z) for a u of mean zero and unit variance.
+ *
+ * us_ffn_gated_fwd:  Z[T,2f] = d^-1/2 X Wgu = [Zg | Zu];  H[T,f] = alpha f(Zg) Zu;  Y[T,d] = fp16(f^-1/2 H Wd)      alpha <= 0: us_gate_scales'
+ *   X [T,d], Wgu [d,2f] (the gate's columns first), Wd [f,d]; T is free (one token upwards, no multiple of anything), d and f are
+ *   multiples of 16 from 16 to US_FFN_GATED_MAX.
+ *   mode: US_FFN_FP8: operands are E4M3 codes (else FP16) and H receives E4M3 codes (else FP16).
+ *   H is made from the FP32 sums and rounded once.  Z is what the backward pass needs: FP16, or with US_FFN_KEEP8 8-bit blocks (us_keep8_store's
+ *   format, also made from the FP32 sums, the blocks of Zg and of Zu starting at their first columns): codes Z [T,2f] and scales Zs
+ *   [T, 2 us_keep8_blocks(f)].  Without US_FFN_KEEP8 Zs is not used and Z may be NULL: nothing is kept (serving).
+ * us_ffn_gated_bwd:  dH = d^-1/2 G Wd^T;  dZ[T,2f] = [beta_gate f'(Zg) Zu dH | beta_up f(Zg) dH];  dX = fp16((2f)^-1/2 dZ Wgu^T);
+ *                    dWgu = fp16(T^-1/2 X^T dZ);  dWd = fp16(T^-1/2 H^T G)
+ *   beta_gate <= 0 selects us_gate_scales' beta, beta_up <= 0 its alpha: either half of dZ then has unit variance on its own (as
+ *   us_linear_scales' mode 0 does for a product).  Both halves meet again in dX and dWgu: for gradients that are a multiple of the loss's
+ *   (X is then no cut-edge, Sec. 5.2 step 2) give both the same factor, such as the geometric mean (alpha beta)^1/2.
+ *   G [T,d] and dZ [T,2f] (out): FP16, or E5M2 codes with US_FFN_FP8; dX [T,d], dWgu [d,2f], dWd [f,d]: FP16 out, each may be NULL
+ *   (skipped).  dH is never stored or rounded.  Zg and Zu are the kept values.  H: without US_FFN_KEEP8 the forward call's; with it,
+ *   scratch that this call fills again from the kept values with the factor alpha (the forward call's H need not live until then).
+ *   With T = 0 the weights' gradients are zeros.
+ * Workspace (16-byte aligned, contents undefined on entry and exit): us_ffn_gated_workspace_bytes serves both; the forward call can do
+ * without (NULL), the backward call needs it where a weight's gradient is cut into slices, as us_linear_bwd does.
+ * Outputs must not overlap inputs or one another.  A gate outside the list is US_ERR_DTYPE, an unknown mode bit US_ERR_VALUE.
+ */
+typedef enum { US_GATE_SILU = 0, US_GATE_GELU = 1, US_GATE_RELU = 2, US_GATE_SIGMOID = 3 } us_gate;
+#define US_FFN_KEEP8 4          /* mode bit of us_ffn_gated_*: Z is kept in 8-bit blocks                     */
+#define US_FFN_GATED_MAX (1 << 20)
+us_status us_gate_scales(us_gate gate, float* alpha, float* beta);      /* host only; host pointers */
+us_status us_ffn_gated_fwd(const void* X, const void* Wgu, const void* Wd, void* Z, void* Zs, void* H, void* Y, long T, long d, long f,
+                           us_gate gate, int mode, float alpha, void* workspace, size_t workspace_bytes, void* stream);
+us_status us_ffn_gated_bwd(const void* X, const void* Wgu, const void* Wd, const void* Z, const void* Zs, void* H, const void* G, void* dZ,
+                           void* dX, void* dWgu, void* dWd, long T, long d, long f, us_gate gate, int mode, float alpha, float beta_gate,
+                           float beta_up, void* workspace, size_t workspace_bytes, void* stream);
+size_t us_ffn_gated_workspace_bytes(long T, long d, long f, int mode);
+
+/*
+ * 8-bit checkpoints: an activation kept between the forward and the backward pass in half of its FP16 bytes.  A row's values in blocks of
+ * 32 (the last one may be shorter) share a step 2^e, the smallest power of two from 2^-24 to 2^9 whose 127.5 steps no magnitude of the
+ * block reaches; a value is held as the whole number of steps nearest to it (ties to even).  Magnitudes from 127.5 * 2^9 on, infinities
+ * among them, are held as 127 steps of their sign; NaN as -128, and does not count for e.
+ *   store: X [rows,n] FP16, rows `ld` elements apart -> codes int8 [rows,n], scales uint8 [rows, us_keep8_blocks(n)] holding e + 127
+ *   load:  the values that the codes stand for, which FP16 holds exactly; elements of X beyond column n of a row are left as they were
+ * n a multiple of 16, ld >= n a multiple of 8; rows is free; all pointers 16-byte aligned.  The error of a value is at most half a
+ * step, below 2^-7 of the block's largest magnitude.  us_keep8_blocks(n) = ceil(n / 32).
+ */
+long us_keep8_blocks(long n);
+us_status us_keep8_store(const void* X, long ld, void* codes, void* scales, long rows, long n, void* stream);
+us_status us_keep8_load(const void* codes, const void* scales, void* X, long ld, long rows, long n, void* stream);
+
+/*
+ * From a fused projection to the heads that us_attention_* take: RMS norm of every query and key head, position rotation, head layout.
+ *   QKV: FP16 [batch * s, ld]: a token's `heads` query heads, then its kv_heads key heads, then its kv_heads value heads, dh values each;
+ *        ld >= (heads + 2 kv_heads) dh, a multiple of 8
+ *   fwd:  x^ = x (mean x^2 + eps)^-1/2 over a head;  q, k = R(w x^), v = x, rounded once to FP16;
+ *         Q, K, V: FP16 [batch * heads, s, dh]; a key or value head is repeated for the heads / kv_heads query heads that share it
+ *         (query head i takes key head i / (heads / kv_heads))
+ *   R turns the pairs (2i, 2i+1) (US_ROPE_NEIGHBOURS) or (i, i + rot/2) (US_ROPE_HALVES) of the first `rot` columns by the angle
+ *         pos[t] * freq[i], i < rot/2: (a, b) -> (a cos - b sin, b cos + a sin); the other columns stay
+ *   bwd:  g = R^-1(dq), likewise k's, whose sharing heads' gradients are added in FP32 and get the factor (heads / kv_heads)^-1/2 (unit
+ *         variance; v's too);  dw = fp16(beta_w sum g x^), beta_w <= 0: (rows)^-1/2 with rows = batch s heads (wq) or batch s kv_heads (wk);
+ *         dx = fp16(rstd (g w - x^ mean(g w x^)))  -> dQKV, laid out as QKV with row pitch ld_d; columns beyond the heads are left as they were
+ * wq, wk: FP16 [dh], or NULL for ones.  pos: int32 [batch * s] (any value), or NULL: the place in the sequence.  freq: double [rot / 2],
+ * radians per position, finite (may be NULL if rot = 0); an angle is exact to 2^-30 of a turn for every position.  dwq, dwk: FP16 [dh]
+ * or NULL.  dh a multiple of 16 up to US_ROPE_HEAD_MAX; rot a multiple of 16 up to dh; kv_heads divides heads <= 65535; eps >= 0 (0: a
+ * head of zeros gives NaN).  The workspace (us_qk_norm_rope_workspace_bytes, 16-byte aligned, undefined on entry and exit) holds partial sums
+ * of the weights' gradients, added in a fixed order.  Outputs must not overlap inputs or one another.
+ */
+typedef enum { US_ROPE_HALVES = 0, US_ROPE_NEIGHBOURS = 1 } us_rope_pairs;
+#define US_ROPE_HEAD_MAX 256
+us_status us_qk_norm_rope_fwd(const void* QKV, long ld, const void* wq, const void* wk, const int* pos, const double* freq, void* Q, void* K,
+                              void* V, long batch, long s, long heads, long kv_heads, long dh, long rot, us_rope_pairs pairs, float eps,
+                              void* stream);
+us_status us_qk_norm_rope_bwd(const void* QKV, long ld, const void* wq, const void* wk, const int* pos, const double* freq, const void* dQ,
+                              const void* dK, const void* dV, void* dQKV, long ld_d, void* dwq, void* dwk, long batch, long s, long heads,
+                              long kv_heads, long dh, long rot, us_rope_pairs pairs, float eps, float beta_wq, float beta_wk, void* workspace,
+                              size_t workspace_bytes, void* stream);
+size_t us_qk_norm_rope_workspace_bytes(long batch, long s, long heads, long kv_heads, long dh);
+
 #ifdef __cplusplus
 }
 #endif

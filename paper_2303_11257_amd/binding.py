@@ -18,6 +18,9 @@ EPI_TABLES_READY = 0x100            # flag for EPI_GELU / EPI_GELU_GRAD: tables 
 FFN_FP8, FFN_TABLES_READY = 1, 2    # mode bits of ffn_fwd / ffn_bwd
 TABLE_AREA_BYTES = 256 * 1024
 HIST_BINS = 35
+GATE_SILU, GATE_GELU, GATE_RELU, GATE_SIGMOID = 0, 1, 2, 3
+FFN_KEEP8 = 4                       # mode bit of ffn_gated_fwd / ffn_gated_bwd, next to FFN_FP8
+ROPE_HALVES, ROPE_NEIGHBOURS = 0, 1
 STATUS = {0: "US_OK", 1: "US_ERR_NULL", 2: "US_ERR_SHAPE", 3: "US_ERR_ALIGN", 4: "US_ERR_DTYPE",
           5: "US_ERR_WORKSPACE", 6: "US_ERR_LAUNCH", 7: "US_ERR_VALUE"}
 
@@ -94,7 +97,21 @@ def lib() -> ctypes.CDLL:
     L.us_ffn_bias_bwd.argtypes = [vp] * 14 + [l, l, l, i, vp, sz, vp]
     L.us_ffn_bias_workspace_bytes.argtypes = [l, l, l]
     L.us_ffn_bias_workspace_bytes.restype = sz
-    for name in ("us_linear_scales", "us_cast_fp8", "us_cast_fp8_batch", "us_linear_fwd", "us_linear_bwd", "us_linear_bwd_noalloc", "us_gelu_fwd", "us_gelu_bwd",
+    L.us_gate_scales.argtypes = [i, fp, fp]
+    L.us_ffn_gated_fwd.argtypes = [vp] * 7 + [l, l, l, i, i, f, vp, sz, vp]
+    L.us_ffn_gated_bwd.argtypes = [vp] * 11 + [l, l, l, i, i, f, f, f, vp, sz, vp]
+    L.us_ffn_gated_workspace_bytes.argtypes = [l, l, l, i]
+    L.us_ffn_gated_workspace_bytes.restype = sz
+    L.us_keep8_blocks.argtypes = [l]
+    L.us_keep8_blocks.restype = l
+    L.us_keep8_store.argtypes = [vp, l, vp, vp, l, l, vp]
+    L.us_keep8_load.argtypes = [vp, vp, vp, l, l, l, vp]
+    L.us_qk_norm_rope_fwd.argtypes = [vp, l] + [vp] * 7 + [l] * 6 + [i, f, vp]
+    L.us_qk_norm_rope_bwd.argtypes = [vp, l] + [vp] * 8 + [l, vp, vp] + [l] * 6 + [i, f, f, f, vp, sz, vp]
+    L.us_qk_norm_rope_workspace_bytes.argtypes = [l] * 5
+    L.us_qk_norm_rope_workspace_bytes.restype = sz
+    for name in ("us_gate_scales", "us_ffn_gated_fwd", "us_ffn_gated_bwd", "us_keep8_store", "us_keep8_load", "us_qk_norm_rope_fwd", "us_qk_norm_rope_bwd",
+                 "us_linear_scales", "us_cast_fp8", "us_cast_fp8_batch", "us_linear_fwd", "us_linear_bwd", "us_linear_bwd_noalloc", "us_gelu_fwd", "us_gelu_bwd",
                  "us_gelu_tables", "us_ffn_fwd", "us_ffn_bwd", "us_weighted_add", "us_ffn_res_fwd", "us_ffn_res_bwd", "us_act_fwd", "us_act_bwd", "us_layer_norm_fwd", "us_layer_norm_bwd", "us_exponent_histogram", "us_cast_snr",
                  "us_linear_bias_fwd", "us_bias_grad", "us_ffn_bias_fwd", "us_ffn_bias_bwd", "us_softmax_fwd", "us_softmax_bwd",
                  "us_softmax_xent", "us_matmul_batched", "us_attention_fwd", "us_attention_bwd", "us_sum_fwd", "us_sum_bwd"):
@@ -358,3 +375,69 @@ def cast_snr(src, src_dt, n, dst_dt, scale, sums, stream=None):
     status = (_lib or lib()).us_cast_snr(src, src_dt, n, dst_dt, scale, sums, stream)
     if status:
         raise UsError(status, "us_cast_snr")
+
+
+def gate_scales(gate: int):
+    """(alpha, beta) of a gate: 1 / rms f(z) for the gated product, 1 / rms f'(z) for the gradient of the gate's input."""
+    a, b = ctypes.c_float(), ctypes.c_float()
+    status = (_lib or lib()).us_gate_scales(gate, ctypes.byref(a), ctypes.byref(b))
+    if status:
+        raise UsError(status, "us_gate_scales")
+    return a.value, b.value
+
+
+def ffn_gated_fwd(X, Wgu, Wd, Z, Zs, H, Y, T, d, f, gate=GATE_SILU, mode=0, workspace=None, workspace_bytes=0, stream=None, alpha=0.0):
+    """mode: FFN_FP8 and FFN_KEEP8.  Z None: nothing is kept for a backward pass; Zs: the scales of 8-bit blocks, else None."""
+    status = (_lib or lib()).us_ffn_gated_fwd(X, Wgu, Wd, Z, Zs, H, Y, T, d, f, gate, int(mode), alpha, workspace, workspace_bytes, stream)
+    if status:
+        raise UsError(status, "us_ffn_gated_fwd")
+
+
+def ffn_gated_bwd(X, Wgu, Wd, Z, Zs, H, G, dZ, dX, dWgu, dWd, T, d, f, gate=GATE_SILU, mode=0, workspace=None, workspace_bytes=0, stream=None,
+                  alpha=0.0, beta_gate=0.0, beta_up=0.0):
+    """With FFN_KEEP8 H is scratch that the call fills from the kept values.  beta_gate = beta_up for gradients of X and Wgu that are a
+    multiple of the loss's (include/us.h)."""
+    status = (_lib or lib()).us_ffn_gated_bwd(X, Wgu, Wd, Z, Zs, H, G, dZ, dX, dWgu, dWd, T, d, f, gate, int(mode), alpha, beta_gate, beta_up,
+                                              workspace, workspace_bytes, stream)
+    if status:
+        raise UsError(status, "us_ffn_gated_bwd")
+
+
+def ffn_gated_workspace_bytes(T: int, d: int, f: int, mode: int = 0) -> int:
+    return int(lib().us_ffn_gated_workspace_bytes(T, d, f, int(mode)))
+
+
+def keep8_blocks(n: int) -> int:
+    return int((_lib or lib()).us_keep8_blocks(n))
+
+
+def keep8_store(X, ld, codes, scales, rows, n, stream=None):
+    """X: FP16 rows `ld` elements apart; codes: int8 [rows, n]; scales: uint8 [rows, keep8_blocks(n)]."""
+    status = (_lib or lib()).us_keep8_store(X, ld, codes, scales, rows, n, stream)
+    if status:
+        raise UsError(status, "us_keep8_store")
+
+
+def keep8_load(codes, scales, X, ld, rows, n, stream=None):
+    status = (_lib or lib()).us_keep8_load(codes, scales, X, ld, rows, n, stream)
+    if status:
+        raise UsError(status, "us_keep8_load")
+
+
+def qk_norm_rope_fwd(QKV, ld, wq, wk, pos, freq, Q, K, V, batch, s, heads, kv_heads, dh, rot, pairs=ROPE_HALVES, eps=0.0, stream=None):
+    """pos: int32 device pointer or None; freq: device pointer to rot / 2 float64, radians per position."""
+    status = (_lib or lib()).us_qk_norm_rope_fwd(QKV, ld, wq, wk, pos, freq, Q, K, V, batch, s, heads, kv_heads, dh, rot, pairs, eps, stream)
+    if status:
+        raise UsError(status, "us_qk_norm_rope_fwd")
+
+
+def qk_norm_rope_bwd(QKV, ld, wq, wk, pos, freq, dQ, dK, dV, dQKV, ld_d, dwq, dwk, batch, s, heads, kv_heads, dh, rot, pairs=ROPE_HALVES, eps=0.0,
+                     beta_wq=0.0, beta_wk=0.0, workspace=None, workspace_bytes=0, stream=None):
+    status = (_lib or lib()).us_qk_norm_rope_bwd(QKV, ld, wq, wk, pos, freq, dQ, dK, dV, dQKV, ld_d, dwq, dwk, batch, s, heads, kv_heads, dh, rot, pairs,
+                                                 eps, beta_wq, beta_wk, workspace, workspace_bytes, stream)
+    if status:
+        raise UsError(status, "us_qk_norm_rope_bwd")
+
+
+def qk_norm_rope_workspace_bytes(batch: int, s: int, heads: int, kv_heads: int, dh: int) -> int:
+    return int(lib().us_qk_norm_rope_workspace_bytes(batch, s, heads, kv_heads, dh))

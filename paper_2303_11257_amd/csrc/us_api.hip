@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "us_device.h"
+#include "us_gate.h"
 #include "us_launch.h"
 
 using namespace us;
@@ -141,10 +142,11 @@ size_t us_workspace_bytes(long b, long m, long n) {
 }
 
 // us_linear_bias_fwd.  launch = false: the argument checks only (what a composite call runs for every one of its
-// products before it enqueues the first, so that a call that fails has touched no device memory).
+// products before it enqueues the first, so that a call that fails has touched no device memory).  any_b: the row count need not be a multiple
+// of 16 (no kernel needs it to be: rows, and the reduction over them, end where the matrix does).
 static us_status linear_fwd_impl(const void* X, const void* W, const void* bias, void* Y, long b, long m, long n, us_dtype x_dt,
                                  us_dtype w_dt, us_dtype y_dt, float alpha, us_epilogue epi, float epi_scale, void* aux16,
-                                 void* aux8, void* workspace, size_t workspace_bytes, void* stream, bool launch) {
+                                 void* aux8, void* workspace, size_t workspace_bytes, void* stream, bool launch, bool any_b = false) {
   const bool tables_ready = ((int)epi & US_EPI_TABLES_READY) != 0;
   const int act = ((int)epi >> 4) & 0xf;
   epi = (us_epilogue)((int)epi & 0xf);
@@ -157,7 +159,7 @@ static us_status linear_fwd_impl(const void* X, const void* W, const void* bias,
   if (epi != US_EPI_NONE && y_dt != US_F16) return US_ERR_DTYPE;
   if (bias && y_dt != US_F16) return US_ERR_DTYPE;       // the bias joins the sum before the rounding to FP16
   if (epi == US_EPI_RESIDUAL && !residual_weight_ok(epi_scale)) return US_ERR_VALUE;
-  if (b < 0 || m < 0 || n < 0 || !mult16(b) || !mult16(m) || !mult16(n)) return US_ERR_SHAPE;
+  if (b < 0 || m < 0 || n < 0 || !(any_b || mult16(b)) || !mult16(m) || !mult16(n)) return US_ERR_SHAPE;
   if (b == 0 || n == 0) return US_OK;
   if (!Y || (m > 0 && (!X || !W))) return US_ERR_NULL;
   if (epi == US_EPI_GELU && !aux16 && !aux8) return US_ERR_NULL;
@@ -210,7 +212,7 @@ us_status us_linear_bias_fwd(const void* X, const void* W, const void* bias, voi
 static us_status linear_bwd_impl(const void* X, const void* W, const void* G, void* dX, void* dW, long b, long m, long n,
                                  us_dtype x_dt, us_dtype w_dt, us_dtype g_dt, us_dtype out_dt, float beta_x, float beta_w,
                                  us_epilogue epi, float epi_scale, const void* Zpre, void* aux8, void* workspace,
-                                 size_t workspace_bytes, void* stream, void* colsum, bool launch = true) {
+                                 size_t workspace_bytes, void* stream, void* colsum, bool launch = true, bool any_b = false) {
   const bool tables_ready = ((int)epi & US_EPI_TABLES_READY) != 0;
   const int act = ((int)epi >> 4) & 0xf;
   epi = (us_epilogue)((int)epi & 0xf);
@@ -222,7 +224,7 @@ static us_status linear_bwd_impl(const void* X, const void* W, const void* G, vo
   if (epi != US_EPI_NONE && epi != US_EPI_GELU_GRAD && epi != US_EPI_RESIDUAL) return US_ERR_DTYPE;
   if (epi != US_EPI_NONE && out_dt != US_F16) return US_ERR_DTYPE;
   if (epi == US_EPI_RESIDUAL && !residual_weight_ok(epi_scale)) return US_ERR_VALUE;
-  if (b < 0 || m < 0 || n < 0 || !mult16(b) || !mult16(m) || !mult16(n)) return US_ERR_SHAPE;
+  if (b < 0 || m < 0 || n < 0 || !(any_b || mult16(b)) || !mult16(m) || !mult16(n)) return US_ERR_SHAPE;
   // with the GELU' epilogue the FP16 result is optional: its E5M2 copy alone may be asked for
   const bool do_dx = (dX || (epi == US_EPI_GELU_GRAD && (aux8 || colsum))) && b > 0 && m > 0;
   const bool do_dw = dW && m > 0 && n > 0;
@@ -698,6 +700,170 @@ us_status us_sum_bwd(const void* G, void* dX, long rows, long n, float beta, voi
   if (!G || !dX) return US_ERR_NULL;
   if (!aligned16(dX) || ((uintptr_t)G & 1)) return US_ERR_ALIGN;
   return from_hip(launch_sum_bwd(G, dX, rows, n, beta > 0.0f ? beta : 1.0f, as_stream(stream)));
+}
+
+// ---- gated feed-forward block ------------------------------------------------------------------------------------------------
+
+us_status us_gate_scales(us_gate gate, float* alpha, float* beta) {
+  if ((int)gate < 0 || (int)gate > 3) return US_ERR_DTYPE;
+  if (!alpha || !beta) return US_ERR_NULL;
+  *alpha = kGateAlpha[gate];
+  *beta = kGateBeta[gate];
+  return US_OK;
+}
+
+size_t us_ffn_gated_workspace_bytes(long T, long d, long f, int mode) {
+  (void)mode;
+  if (T < 1 || d < 1 || f < 1) return 0;
+  const size_t a = us_workspace_bytes(T, f, d), b = us_workspace_bytes(T, d, 2 * f);      // dWd and dWgu
+  return a > b ? a : b;
+}
+
+// What both directions check first.  The rows of Z and Wgu bound f: the kernels address a tile with 32-bit offsets.
+static us_status gated_shape(long T, long d, long f, us_gate gate, int mode) {
+  if ((int)gate < 0 || (int)gate > 3) return US_ERR_DTYPE;
+  if (mode & ~(US_FFN_FP8 | US_FFN_KEEP8)) return US_ERR_VALUE;
+  if (T < 0 || d < 16 || f < 16 || !mult16(d) || !mult16(f) || d > US_FFN_GATED_MAX || f > US_FFN_GATED_MAX) return US_ERR_SHAPE;
+  return US_OK;
+}
+
+us_status us_ffn_gated_fwd(const void* X, const void* Wgu, const void* Wd, void* Z, void* Zs, void* H, void* Y, long T, long d, long f,
+                           us_gate gate, int mode, float alpha, void* workspace, size_t workspace_bytes, void* stream) {
+  const CallScope scope;
+  if (us_status s = gated_shape(T, d, f, gate, mode); s != US_OK) return s;
+  const bool fp8 = (mode & US_FFN_FP8) != 0, keep8 = (mode & US_FFN_KEEP8) != 0;
+  if (T == 0) return US_OK;
+  if (!X || !Wgu || !Wd || !H || !Y || (keep8 && (!Z || !Zs))) return US_ERR_NULL;
+  if (!aligned16(X) || !aligned16(Wgu) || !aligned16(Wd) || !aligned16(Z) || !aligned16(Zs) || !aligned16(H) || !aligned16(Y) || !aligned16(workspace))
+    return US_ERR_ALIGN;
+  (void)workspace_bytes;
+  const us_dtype op = fp8 ? US_E4M3 : US_F16;
+  GemmProblem p{};
+  p.A = X; p.B = Wgu; p.C = Z;
+  p.M = T; p.N = 2 * f; p.K = d;
+  p.lda = d; p.ldb = 2 * f; p.ldc = 2 * f;
+  p.a_kc = true; p.b_kc = false;
+  p.a_dt = op; p.b_dt = op; p.c_dt = US_F16;
+  p.scale = (float)(1.0 / sqrt((double)d));
+  p.epi_scale = alpha > 0.0f ? alpha : kGateAlpha[gate];
+  p.act = (int)gate;
+  p.keep_scale = Zs;
+  p.gate_h = H;
+  if (!gemm_gate_offsets_fit(p)) return US_ERR_SHAPE;
+  if (us_status s = from_hip(gemm_gate_fwd(p, keep8, as_stream(stream))); s != US_OK) return s;
+  return linear_fwd_impl(H, Wd, nullptr, Y, T, f, d, op, op, US_F16, 0.0f, US_EPI_NONE, 0.0f, nullptr, nullptr, nullptr, 0, stream, true, true);
+}
+
+us_status us_ffn_gated_bwd(const void* X, const void* Wgu, const void* Wd, const void* Z, const void* Zs, void* H, const void* G, void* dZ,
+                           void* dX, void* dWgu, void* dWd, long T, long d, long f, us_gate gate, int mode, float alpha, float beta_gate,
+                           float beta_up, void* workspace, size_t workspace_bytes, void* stream) {
+  const CallScope scope;
+  if (us_status s = gated_shape(T, d, f, gate, mode); s != US_OK) return s;
+  const bool fp8 = (mode & US_FFN_FP8) != 0, keep8 = (mode & US_FFN_KEEP8) != 0;
+  if (T > 0 && (!X || !Wgu || !Wd || !Z || !H || !G || !dZ || (keep8 && !Zs))) return US_ERR_NULL;
+  if (!aligned16(X) || !aligned16(Wgu) || !aligned16(Wd) || !aligned16(Z) || !aligned16(Zs) || !aligned16(H) || !aligned16(G) || !aligned16(dZ) ||
+      !aligned16(dX) || !aligned16(dWgu) || !aligned16(dWd) || !aligned16(workspace))
+    return US_ERR_ALIGN;
+  const us_dtype op = fp8 ? US_E4M3 : US_F16, gr = fp8 ? US_E5M2 : US_F16;
+  GemmProblem p{};
+  p.A = G; p.B = Wd; p.C = fp8 ? nullptr : dZ;
+  p.M = T; p.N = f; p.K = d;
+  p.lda = d; p.ldb = d; p.ldc = 2 * f;
+  p.a_kc = true; p.b_kc = true;
+  p.a_dt = gr; p.b_dt = op; p.c_dt = US_F16;
+  p.scale = (float)(1.0 / sqrt((double)d));
+  p.epi_scale = beta_gate > 0.0f ? beta_gate : kGateBeta[gate];
+  p.skip_scale = beta_up > 0.0f ? beta_up : kGateAlpha[gate];
+  p.gate_alpha = alpha > 0.0f ? alpha : kGateAlpha[gate];
+  p.act = (int)gate;
+  p.Zpre = Z;
+  p.keep_scale = const_cast<void*>(Zs);
+  p.gate_h = H;
+  p.aux8 = fp8 ? dZ : nullptr;
+  if (!gemm_gate_offsets_fit(p)) return US_ERR_SHAPE;
+  for (int pass = 0; pass < 2; ++pass) {      // pass 0 checks the layers' products, pass 1 launches
+    const bool go = pass == 1;
+    if (go && T > 0) {
+      if (us_status s = from_hip(gemm_gate_grad(p, keep8, as_stream(stream))); s != US_OK) return s;
+    }
+    // dWd = T^-1/2 H^T G; dX = (2f)^-1/2 dZ Wgu^T and dWgu = T^-1/2 X^T dZ (no tokens: gradients of zero)
+    us_status s = linear_bwd_impl(H, Wd, G, nullptr, dWd, T, f, d, op, op, gr, US_F16, 0.0f, 0.0f, US_EPI_NONE, 0.0f, nullptr, nullptr, workspace,
+                                  workspace_bytes, stream, nullptr, go, true);
+    if (s != US_OK) return s;
+    s = linear_bwd_impl(X, Wgu, dZ, dX, dWgu, T, d, 2 * f, op, op, gr, US_F16, 0.0f, 0.0f, US_EPI_NONE, 0.0f, nullptr, nullptr, workspace,
+                        workspace_bytes, stream, nullptr, go, true);
+    if (s != US_OK) return s;
+  }
+  return US_OK;
+}
+
+// ---- 8-bit checkpoints ----------------------------------------------------------------------------------------------------------
+
+long us_keep8_blocks(long n) { return n < 1 ? 0 : (n + 31) / 32; }
+
+static us_status keep8_checks(const void* x, long ld, const void* codes, const void* scales, long rows, long n) {
+  if (rows < 0 || n < 0 || !mult16(n) || n > (1L << 30) || ld < n || ld % 8 != 0) return US_ERR_SHAPE;
+  if (rows == 0 || n == 0) return US_OK;
+  if (!x || !codes || !scales) return US_ERR_NULL;
+  if (!aligned16(x) || !aligned16(codes) || !aligned16(scales)) return US_ERR_ALIGN;
+  return US_OK;
+}
+
+us_status us_keep8_store(const void* X, long ld, void* codes, void* scales, long rows, long n, void* stream) {
+  if (us_status s = keep8_checks(X, ld, codes, scales, rows, n); s != US_OK) return s;
+  if (rows == 0 || n == 0) return US_OK;
+  return from_hip(launch_keep8_store(X, ld, codes, scales, rows, n, as_stream(stream)));
+}
+
+us_status us_keep8_load(const void* codes, const void* scales, void* X, long ld, long rows, long n, void* stream) {
+  if (us_status s = keep8_checks(X, ld, codes, scales, rows, n); s != US_OK) return s;
+  if (rows == 0 || n == 0) return US_OK;
+  return from_hip(launch_keep8_load(codes, scales, X, ld, rows, n, as_stream(stream)));
+}
+
+// ---- queries, keys and values into heads ------------------------------------------------------------------------------------------
+
+static us_status heads_shape(long batch, long s, long heads, long kv_heads, long dh, long rot, us_rope_pairs pairs, float eps) {
+  if (batch < 0 || s < 0 || batch > (1L << 31) - 1 || s > (1L << 31) - 1 || heads < 1 || kv_heads < 1 || heads > 65535 || heads % kv_heads != 0) return US_ERR_SHAPE;
+  if (dh < 16 || dh > US_ROPE_HEAD_MAX || !mult16(dh) || rot < 0 || rot > dh || !mult16(rot)) return US_ERR_SHAPE;
+  if (pairs != US_ROPE_HALVES && pairs != US_ROPE_NEIGHBOURS) return US_ERR_VALUE;
+  if (!(eps >= 0.0f)) return US_ERR_VALUE;
+  return US_OK;
+}
+
+us_status us_qk_norm_rope_fwd(const void* QKV, long ld, const void* wq, const void* wk, const int* pos, const double* freq, void* Q, void* K,
+                              void* V, long batch, long s, long heads, long kv_heads, long dh, long rot, us_rope_pairs pairs, float eps, void* stream) {
+  if (us_status e = heads_shape(batch, s, heads, kv_heads, dh, rot, pairs, eps); e != US_OK) return e;
+  if (ld < (heads + 2 * kv_heads) * dh || ld % 8 != 0) return US_ERR_SHAPE;
+  if (batch == 0 || s == 0) return US_OK;
+  if (!QKV || !Q || !K || !V || (rot > 0 && !freq)) return US_ERR_NULL;
+  if (!aligned16(QKV) || !aligned16(wq) || !aligned16(wk) || !aligned16(Q) || !aligned16(K) || !aligned16(V) || ((uintptr_t)pos & 3) || ((uintptr_t)freq & 7))
+    return US_ERR_ALIGN;
+  return from_hip(launch_heads_fwd(HeadsCall{QKV, wq, wk, pos, freq, ld, batch, s, heads, kv_heads, dh, rot, (int)pairs, eps}, Q, K, V, as_stream(stream)));
+}
+
+size_t us_qk_norm_rope_workspace_bytes(long batch, long s, long heads, long kv_heads, long dh) {
+  (void)heads, (void)kv_heads;
+  return (batch < 1 || s < 1 || dh < 1) ? 0 : heads_workspace_bytes(batch * s, dh);
+}
+
+us_status us_qk_norm_rope_bwd(const void* QKV, long ld, const void* wq, const void* wk, const int* pos, const double* freq, const void* dQ,
+                              const void* dK, const void* dV, void* dQKV, long ld_d, void* dwq, void* dwk, long batch, long s, long heads,
+                              long kv_heads, long dh, long rot, us_rope_pairs pairs, float eps, float beta_wq, float beta_wk, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  if (us_status e = heads_shape(batch, s, heads, kv_heads, dh, rot, pairs, eps); e != US_OK) return e;
+  const long columns = (heads + 2 * kv_heads) * dh;
+  if (ld < columns || ld % 8 != 0 || ld_d < columns || ld_d % 8 != 0) return US_ERR_SHAPE;
+  if (batch == 0 || s == 0) return US_OK;
+  if (!QKV || !dQ || !dK || !dV || !dQKV || (rot > 0 && !freq)) return US_ERR_NULL;
+  if (!aligned16(QKV) || !aligned16(wq) || !aligned16(wk) || !aligned16(dQ) || !aligned16(dK) || !aligned16(dV) || !aligned16(dQKV) || !aligned16(workspace) ||
+      ((uintptr_t)dwq & 1) || ((uintptr_t)dwk & 1) || ((uintptr_t)pos & 3) || ((uintptr_t)freq & 7))
+    return US_ERR_ALIGN;
+  if (!workspace || workspace_bytes < heads_workspace_bytes(batch * s, dh)) return US_ERR_WORKSPACE;
+  if (!(beta_wq > 0.0f)) beta_wq = (float)(1.0 / sqrt((double)batch * (double)s * (double)heads));
+  if (!(beta_wk > 0.0f)) beta_wk = (float)(1.0 / sqrt((double)batch * (double)s * (double)kv_heads));
+  return from_hip(launch_heads_bwd(HeadsCall{QKV, wq, wk, pos, freq, ld, batch, s, heads, kv_heads, dh, rot, (int)pairs, eps}, dQ, dK, dV, dQKV, ld_d, dwq, dwk,
+                                   beta_wq, beta_wk, workspace, as_stream(stream)));
 }
 
 }  // extern "C"

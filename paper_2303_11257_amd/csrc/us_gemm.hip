@@ -56,7 +56,7 @@ void note_gemm_launch(const char* kind, int bm, int bn, int waves_k, int nst, bo
 
 const char* last_launch_record() {
   static const char* const epi_name[] = {"store", "act", "act_grad", "partial", "gelu_tab", "gelu_grad_tab", "gelu_tab16", "residual",
-                                         "softmax", "softmax_grad"};
+                                         "softmax", "softmax_grad", "gate", "gate8", "gate_grad", "gate8_grad"};
   int len = 0;
   g_record[0] = 0;
   for (int i = 0; i < g_note_count; ++i) {
@@ -66,7 +66,7 @@ const char* last_launch_record() {
     if (n.waves > 0) snprintf(waves, sizeof(waves), ":w%d", n.waves);
     const int w = snprintf(g_record + len, (size_t)room, "%s%s:%dx%d:wk%d:st%d:%s:%s:%s%s:s%d%s", i ? " + " : "", n.kind, n.bm, n.bn, n.waves_k,
                            n.nst, n.fp8 ? "fp8" : "f16", n.a_kc ? (n.b_kc ? "NT" : "NN") : (n.b_kc ? "TT" : "TN"),
-                           (n.epi >= 0 && n.epi < 10) ? epi_name[n.epi] : "?", n.wide ? ":f32" : "", n.splits, waves);
+                           (n.epi >= 0 && n.epi < 14) ? epi_name[n.epi] : "?", n.wide ? ":f32" : "", n.splits, waves);
     if (w < 0 || w >= room) break;
     len += w;
   }
@@ -119,6 +119,19 @@ int gemm_splits(long M, long N, long K) {
 size_t gemm_workspace_bytes(long M, long N, long K) {
   const int s = gemm_splits(M, N, K);
   return s <= 1 ? 0 : (size_t)s * (size_t)M * (size_t)N * sizeof(float);
+}
+
+hipError_t gemm_gate_fwd_f16(const GemmProblem& p, bool keep8, hipStream_t st);
+hipError_t gemm_gate_fwd_fp8(const GemmProblem& p, bool keep8, hipStream_t st);
+hipError_t gemm_gate_grad_f16(const GemmProblem& p, bool keep8, hipStream_t st);
+hipError_t gemm_gate_grad_fp8(const GemmProblem& p, bool keep8, hipStream_t st);
+
+bool gemm_gate_offsets_fit(const GemmProblem& p) { return offsets_fit(p); }
+hipError_t gemm_gate_fwd(const GemmProblem& p, bool keep8, hipStream_t st) {
+  return p.a_dt == US_F16 ? gemm_gate_fwd_f16(p, keep8, st) : gemm_gate_fwd_fp8(p, keep8, st);
+}
+hipError_t gemm_gate_grad(const GemmProblem& p, bool keep8, hipStream_t st) {
+  return p.a_dt == US_F16 ? gemm_gate_grad_f16(p, keep8, st) : gemm_gate_grad_fp8(p, keep8, st);
 }
 
 hipError_t launch_gemm(const GemmProblem& p, hipStream_t st) {

@@ -13,9 +13,10 @@ namespace us {
 // taken from a table over the FP16 pre-activation that the workgroup copies into LDS.
 // EPI_GELU_TAB16: EPI_GELU with an FP16 activation output (and optionally its FP8 copy), from a table.
 // EPI_RESIDUAL: C = fp16( skip_scale * R + epi_scale * fp16(scale * acc) ), R an FP16 [M,N] input (Zpre).
+// EPI_GATE..: the gated block's (us_gemm_gate.h); their numbers continue behind NOTE_SOFTMAX_GRAD (us_launch.h).
 enum GemmEpi : int {
   EPI_STORE = 0, EPI_GELU = 1, EPI_GELU_GRAD = 2, EPI_PARTIAL = 3, EPI_GELU_TAB = 4, EPI_GELU_GRAD_TAB = 5, EPI_GELU_TAB16 = 6,
-  EPI_RESIDUAL = 7
+  EPI_RESIDUAL = 7, EPI_GATE = 10, EPI_GATE8 = 11, EPI_GATE_GRAD = 12, EPI_GATE8_GRAD = 13
 };
 
 // Division of an unsigned 32-bit number by a divisor that the host knows (Granlund & Montgomery, round-up method): one high
@@ -115,6 +116,9 @@ struct GemmArgs {
   long batch_a, batch_b, batch_c;   // bytes between consecutive problems of a batch (blockIdx.z), 0 for a single one
   const _Float16* bias;  // forward product only: optional row [N] added to scale * acc before the rounding, or NULL
   float* colsum;         // EPI_GELU_GRAD / _TAB: optional FP32 [ceil(M / 32)][N], column sums of the FP16 result per 32-row block
+  uint8_t* keep_scale;   // EPI_GATE8, _GRAD: scales of the 8-bit blocks, [M][2 * ceil(f / 32)]
+  void* gate_h;          // EPI_GATE..: H [M][f]
+  float gate_alpha;      // EPI_GATE8_GRAD: H's factor (epi_scale, skip_scale: those of dZ's halves)
 };
 
 // Problem number blockIdx.z of a batch of equally shaped, independent products (plain-store epilogue only).

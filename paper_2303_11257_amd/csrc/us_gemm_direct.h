@@ -30,6 +30,7 @@
 #include <utility>
 
 #include "us_gemm_common.h"
+#include "us_gemm_gate.h"
 
 namespace us {
 
@@ -56,6 +57,7 @@ struct DirectTile {
   static constexpr int REDUCE_BYTES = Cfg::WAVES_K == 1 ? 0 : Cfg::WAVES * (Cfg::FM / 2) * Cfg::FN * 16 * 64 * 4;
   static constexpr int STRIP_TABLE_BYTES = EpiStrip<Cfg, WIDE, EPI>::BYTES;
   static constexpr int EPI_BYTES = REDUCE_BYTES > STRIP_TABLE_BYTES ? REDUCE_BYTES : STRIP_TABLE_BYTES;
+  static_assert(!(is_gate(EPI) || is_gate_grad(EPI)) || GateStrip<Cfg, FP8, EPI>::BYTES <= RING_BYTES, "the gated block's strips lie in the ring");
   static constexpr int LDS_BYTES = RING_BYTES > EPI_BYTES ? RING_BYTES : EPI_BYTES;
   static_assert(A_BYTES % (16 * Cfg::THREADS) == 0 && B_BYTES % (16 * Cfg::THREADS) == 0, "whole wave loads only");
   static_assert(Cfg::NST >= 2 && Cfg::NST <= 5, "");
@@ -149,6 +151,18 @@ struct OperandLoads {
     for (int j = 0; j < NL; ++j) {
       const int r = KC ? lds_row(j) : chunk(j) * (16 / ES);
       off[j] = (row0 + r < extent_r) ? (uint32_t)lds_row(j) * (uint32_t)(ld * ES) + (uint32_t)chunk(j) * 16u : kOutOfRange;
+    }
+  }
+  // B of the gated block's forward product, K-strided [k][2f]: the tile's columns, in parts of PART, are by turns the columns from `col0` on of the
+  // gate's half and the same ones of the other half
+  template <int PART>
+  __device__ __forceinline__ void init_gate(const uint8_t* base, long ld, long col0, long f, long k0) {
+    static_assert(!KC && PART % 16 == 0, "");
+    next = base + (k0 * ld + col0) * ES;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int c = chunk(j) * (16 / ES), col = c / (2 * PART) * PART + c % PART;
+      off[j] = (col0 + col < f) ? (uint32_t)lds_row(j) * (uint32_t)(ld * ES) + (uint32_t)(col + (c / PART % 2 ? f : 0)) * ES : kOutOfRange;
     }
   }
   // the last stage holds only `krem` elements of the reduction
@@ -380,7 +394,8 @@ __device__ __forceinline__ void gemm_direct_tile(const GemmArgs& g, int bid, lon
   OperandLoads<THREADS, BM, BKB, A_KC, FP8, PA, T::A_LOADS, T::M16> la;
   OperandLoads<THREADS, BN, BKB, B_KC, FP8, PB, T::B_LOADS, T::M16> lb;
   la.init(g.A, g.lda, m0, g.M, k_begin);
-  lb.init(g.B, g.ldb, n0, g.N, k_begin);
+  if constexpr (is_gate(EPI)) lb.template init_gate<Cfg::WN / 2>(g.B, g.ldb, n0 / 2, g.N / 2, k_begin);
+  else lb.init(g.B, g.ldb, n0, g.N, k_begin);
   const long advA = A_KC ? (long)BKB : (long)T::BK * g.lda * ES;   // bytes per stage
   const long advB = B_KC ? (long)BKB : (long)T::BK * g.ldb * ES;
 
@@ -425,6 +440,22 @@ __device__ __forceinline__ void gemm_direct_tile(const GemmArgs& g, int bid, lon
           const long n = n0 + wn0 + (u % LPR) * 64;
           if (u < ROWS * LPR && m < g.M && n < g.N)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(g.Zpre + m * g.ldc + n),
+                                             US_LDS_PTR(void, dump), 4, 0, 0);
+        }
+      }
+    } else if constexpr (is_gate_grad(EPI)) {
+      // ... of Zg and Zu alike
+      if (s + NST == nstages) {
+        constexpr int ZES = EPI == EPI_GATE8_GRAD ? 1 : 2, ROWS = Cfg::WM / Cfg::WAVES_K, LPR = (Cfg::WN * ZES + 127) / 128;
+        const int lane = threadIdx.x & 63;
+        uint8_t* dump = freed + wave * 256;
+#pragma unroll
+        for (int t = 0; t < 2 * ROWS * LPR; t += 64) {
+          const int u = t + lane, half = u / (ROWS * LPR), v = u % (ROWS * LPR);
+          const long m = m0 + wm0 + wk * ROWS + v / LPR;
+          const long n = n0 + wn0 + v % LPR * (128 / ZES);
+          if (half < 2 && m < g.M && n < g.N)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((const uint8_t*)g.Zpre + (m * g.ldc + half * g.N + n) * ZES),
                                              US_LDS_PTR(void, dump), 4, 0, 0);
         }
       }
@@ -701,11 +732,19 @@ __device__ __forceinline__ void gemm_direct_tile(const GemmArgs& g, int bid, lon
     if (wk == 0) receive(std::integral_constant<int, 0>{});
     else receive(std::integral_constant<int, HALF>{});
     __syncthreads();     // everything exchanged: the strips may overlay the exchange area
-    if (wk == 0) store_block_epilogue<Cfg, EPI, WIDE, 0, HALF, epilogue_takes_bias<A_KC, B_KC, EPI, WIDE>()>(g, acc, lds, m0, n0, split);
+    if constexpr (is_gate(EPI)) {
+      if (wk == 0) gate_epilogue<Cfg, FP8, EPI, 0, HALF>(g, acc, lds, m0, tn);
+      else gate_epilogue<Cfg, FP8, EPI, HALF, FM>(g, acc, lds, m0, tn);
+    } else if constexpr (is_gate_grad(EPI)) {
+      if (wk == 0) gate_grad_epilogue<Cfg, FP8, EPI, 0, HALF>(g, acc, lds, m0, n0);
+      else gate_grad_epilogue<Cfg, FP8, EPI, HALF, FM>(g, acc, lds, m0, n0);
+    } else if (wk == 0) store_block_epilogue<Cfg, EPI, WIDE, 0, HALF, epilogue_takes_bias<A_KC, B_KC, EPI, WIDE>()>(g, acc, lds, m0, n0, split);
     else store_block_epilogue<Cfg, EPI, WIDE, HALF, FM, epilogue_takes_bias<A_KC, B_KC, EPI, WIDE>()>(g, acc, lds, m0, n0, split);
     return;
   }
-  store_block_epilogue<Cfg, EPI, WIDE, 0, Cfg::FM, epilogue_takes_bias<A_KC, B_KC, EPI, WIDE>()>(g, acc, lds, m0, n0, split);
+  if constexpr (is_gate(EPI)) gate_epilogue<Cfg, FP8, EPI, 0, Cfg::FM>(g, acc, lds, m0, tn);
+  else if constexpr (is_gate_grad(EPI)) gate_grad_epilogue<Cfg, FP8, EPI, 0, Cfg::FM>(g, acc, lds, m0, n0);
+  else store_block_epilogue<Cfg, EPI, WIDE, 0, Cfg::FM, epilogue_takes_bias<A_KC, B_KC, EPI, WIDE>()>(g, acc, lds, m0, n0, split);
 }
 
 template <class Cfg, bool FP8, int FA, int FB, bool A_KC, bool B_KC, int EPI, bool WIDE>

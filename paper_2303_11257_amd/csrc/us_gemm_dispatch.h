@@ -156,6 +156,9 @@ inline GemmArgs make_args(const GemmProblem& p, long k_per_split, int BM, int BN
   g.table = (const uint8_t*)p.table;
   g.bias = (const _Float16*)p.bias;
   g.colsum = (float*)p.colsum;
+  g.keep_scale = (uint8_t*)p.keep_scale;
+  g.gate_h = p.gate_h;
+  g.gate_alpha = p.gate_alpha;
   if (p.batch > 1) {
     const long es = (p.a_dt == US_F16) ? 2 : 1;
     g.batch_a = p.batch_a * es;

@@ -1,0 +1,13 @@
+// GEMM family: the gated block's forward product with both halves of Wgu, and dH with the gate's gradient.
+#include "us_gemm_gate_dispatch.h"
+
+namespace us {
+
+hipError_t gemm_gate_fwd_fp8(const GemmProblem& p, bool keep8, hipStream_t st) {
+  return keep8 ? launch_gate<true, false, EPI_GATE8>(p, st) : launch_gate<true, false, EPI_GATE>(p, st);
+}
+hipError_t gemm_gate_grad_fp8(const GemmProblem& p, bool keep8, hipStream_t st) {
+  return keep8 ? launch_gate<true, true, EPI_GATE8_GRAD>(p, st) : launch_gate<true, true, EPI_GATE_GRAD>(p, st);
+}
+
+}  // namespace us

@@ -59,7 +59,8 @@ __device__ __forceinline__ void gemm_small_tile(const GemmArgs& g, int bid, uint
   OperandLoads<64, BM, Cfg::BKB, A_KC, FP8, T::PA, T::A_LOADS, M16> la;
   OperandLoads<64, BN, Cfg::BKB, B_KC, FP8, T::PB, T::B_LOADS, M16> lb;
   la.init(g.A, g.lda, m0, g.M, (long)wave * T::BK);
-  lb.init(g.B, g.ldb, n0, g.N, (long)wave * T::BK);
+  if constexpr (is_gate(EPI)) lb.template init_gate<BN / 2>(g.B, g.ldb, n0 / 2, g.N / 2, (long)wave * T::BK);
+  else lb.init(g.B, g.ldb, n0, g.N, (long)wave * T::BK);
   const long advA = W * (A_KC ? (long)Cfg::BKB : (long)T::BK * g.lda * T::ES);
   const long advB = W * (B_KC ? (long)Cfg::BKB : (long)T::BK * g.ldb * T::ES);
   long kleft = g.K - (long)wave * T::BK;          // elements of the reduction from the next stage to request on
@@ -137,6 +138,31 @@ __device__ __forceinline__ void gemm_small_tile(const GemmArgs& g, int bid, uint
       for (int q = 0; q < 4; ++q)
         *US_LDS_PTR(v4f, part + (wave * BM + i * 32 + Acc::row(q, lane)) * T::RP + j * 32 + Acc::col(q, lane)) = acc.quad(i, j, q);
   __syncthreads();
+  if constexpr (is_gate(EPI) || is_gate_grad(EPI)) {
+    // eight columns of a row per thread: of both halves, or of dH
+    constexpr int HALVES = is_gate(EPI) ? 2 : 1, TPR = BN / 8 / HALVES;
+    const int row = (int)threadIdx.x / TPR, c8 = (int)threadIdx.x % TPR * 8;
+    const long m = m0 + row, n = n0 / HALVES + c8;
+    if (row >= BM || m >= g.M) return;
+    float v[HALVES][8];
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      v4f lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const float* p = part + (w * BM + row) * T::RP + h * (BN / 2) + c8;
+        lo += *US_LDS_PTR(const v4f, p);
+        hi += *US_LDS_PTR(const v4f, p + 4);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[h][k] = (k < 4 ? lo[k & 3] : hi[k & 3]) * g.scale;
+    }
+    with_gate(g.act, [&](auto gate) {
+      if constexpr (is_gate(EPI)) gate_point<EPI, FP8, decltype(gate)::value>(g, m, n, n < g.N / 2, v[0], v[HALVES - 1]);
+      else if (n < g.N) gate_grad_point<EPI, FP8, decltype(gate)::value>(g, m, n, v[0]);
+    });
+    return;
+  }
   const int row = (int)threadIdx.x / (BN / 8), c8 = (int)threadIdx.x % (BN / 8) * 8;
   const long m = m0 + row, n = n0 + c8;
   constexpr bool NEEDS_Z = EPI == EPI_GELU_GRAD || EPI == EPI_RESIDUAL;

@@ -1,0 +1,88 @@
+// 8-bit checkpoints of FP16 activations: rows in blocks of 32 values that share a power of two (us_gate.h says how a block is held).
+// Bound: HBM, 2 + 1 + 1/32 bytes a value in either direction.  A thread holds 8 consecutive values, four neighbouring lanes a block, so the
+// block's largest magnitude takes two exchanges inside a quad of lanes.
+#include <type_traits>
+
+#include "us_gate.h"
+#include "us_launch.h"
+#include "us_rows.h"
+
+namespace us {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// largest of the four lanes of a quad; a NaN does not count
+__device__ __forceinline__ float quad_max(float v) {
+  v = __builtin_fmaxf(v, lane_dpp<0xB1>(v));
+  return __builtin_fmaxf(v, lane_dpp<0x4E>(v));
+}
+
+// One row of chunks (8 values) per blockIdx.y step; lanes beyond the row hold zeros, so a last block of 16 values is a block of 32.
+__global__ void __launch_bounds__(kThreads) keep8_store_kernel(const _Float16* __restrict__ X, long ld, int8_t* __restrict__ codes,
+                                                               uint8_t* __restrict__ scales, long rows, int n, int blocks) {
+  const int chunk = (int)(blockIdx.x * kThreads + threadIdx.x), col = chunk * 8;
+  for (long r = blockIdx.y; r < rows; r += gridDim.y) {
+    v8h x = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (col < n) x = *reinterpret_cast<const v8h*>(X + r * ld + col);
+    float m = 0.0f;
+    bool rare = false;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      m = __builtin_fmaxf(m, __builtin_fabsf((float)x[k]));
+      rare |= x[k] != x[k];
+    }
+    m = quad_max(m);
+    const uint32_t s = keep_scale(m);
+    const float inv = keep_inverse(s);
+    v2i c;
+    if (rare || m >= kKeepClip) {
+      c.x = keep_codes_any((float)x[0], (float)x[1], (float)x[2], (float)x[3], inv);
+      c.y = keep_codes_any((float)x[4], (float)x[5], (float)x[6], (float)x[7], inv);
+    } else {
+      c.x = keep_codes((float)x[0], (float)x[1], (float)x[2], (float)x[3], inv);
+      c.y = keep_codes((float)x[4], (float)x[5], (float)x[6], (float)x[7], inv);
+    }
+    if (col < n) {
+      *reinterpret_cast<v2i*>(codes + r * n + col) = c;
+      if ((chunk & 3) == 0) scales[r * blocks + (chunk >> 2)] = (uint8_t)s;
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) keep8_load_kernel(const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                              _Float16* __restrict__ X, long ld, long rows, int n, int blocks) {
+  const int chunk = (int)(blockIdx.x * kThreads + threadIdx.x), col = chunk * 8;
+  if (col >= n) return;
+  for (long r = blockIdx.y; r < rows; r += gridDim.y) {
+    const v2i c = *reinterpret_cast<const v2i*>(codes + r * n + col);
+    const float step = keep_step(scales[r * blocks + (chunk >> 2)]);
+    v8h x = {(_Float16)keep_value<0>(c.x, step), (_Float16)keep_value<1>(c.x, step), (_Float16)keep_value<2>(c.x, step), (_Float16)keep_value<3>(c.x, step),
+             (_Float16)keep_value<0>(c.y, step), (_Float16)keep_value<1>(c.y, step), (_Float16)keep_value<2>(c.y, step), (_Float16)keep_value<3>(c.y, step)};
+    if (keep_has_nan(c.x) || keep_has_nan(c.y)) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (((k < 4 ? c.x : c.y) >> (k % 4 * 8) & 0xff) == 0x80) x[k] = half_from_bits(0x7e00);
+    }
+    *reinterpret_cast<v8h*>(X + r * ld + col) = x;
+  }
+}
+
+dim3 grid_of(long rows, long n) {
+  const long x = (n / 8 + kThreads - 1) / kThreads;
+  return dim3((unsigned)x, (unsigned)(rows < 65535 ? rows : 65535));
+}
+
+}  // namespace
+
+hipError_t launch_keep8_store(const void* X, long ld, void* codes, void* scales, long rows, long n, hipStream_t st) {
+  keep8_store_kernel<<<grid_of(rows, n), kThreads, 0, st>>>((const _Float16*)X, ld, (int8_t*)codes, (uint8_t*)scales, rows, (int)n, (int)((n + 31) / 32));
+  return hipGetLastError();
+}
+hipError_t launch_keep8_load(const void* codes, const void* scales, void* X, long ld, long rows, long n, hipStream_t st) {
+  keep8_load_kernel<<<grid_of(rows, n), kThreads, 0, st>>>((const int8_t*)codes, (const uint8_t*)scales, (_Float16*)X, ld, rows, (int)n, (int)((n + 31) / 32));
+  return hipGetLastError();
+}
+
+}  // namespace us

@@ -99,6 +99,23 @@ bool attention_merged_gradients_ok(const void* Q, const void* P, const void* dO,
                                    const void* dK, const void* dV, long heads, long s, long d);
 hipError_t launch_attention_rows(bool bwd, const void* X, const void* Y, const void* W, const void* A, void* S, void* P, void* out,
                                  long heads, long s, long d, float scale_s, float scale_row, float scale_out, hipStream_t stream);
+hipError_t launch_keep8_store(const void* X, long ld, void* codes, void* scales, long rows, long n, hipStream_t stream);
+hipError_t launch_keep8_load(const void* codes, const void* scales, void* X, long ld, long rows, long n, hipStream_t stream);
+
+// Queries, keys and values on their way from the fused projection into attention's heads, and their gradients back (us_heads.hip).
+struct HeadsCall {
+  const void *QKV, *wq, *wk;
+  const int* pos;
+  const double* freq;
+  long ld, batch, s, heads, kv_heads, dh, rot;
+  int pairs;
+  float eps;
+};
+size_t heads_workspace_bytes(long tokens, long dh);
+hipError_t launch_heads_fwd(const HeadsCall& c, void* Q, void* K, void* V, hipStream_t stream);
+hipError_t launch_heads_bwd(const HeadsCall& c, const void* dQ, const void* dK, const void* dV, void* dQKV, long ld_dx, void* dwq, void* dwk,
+                            float beta_wq, float beta_wk, void* workspace, hipStream_t stream);
+
 size_t bias_grad_workspace_bytes(long b, long n);
 hipError_t launch_bias_grad(const void* G, us_dtype g_dt, void* dc, long b, long n, float beta, void* workspace, hipStream_t stream);
 // second half of launch_bias_grad alone: dc = fp16(beta * sum over the nblocks rows of partial[nblocks][n])
@@ -133,6 +150,9 @@ struct GemmProblem {
   const void* bias;        // forward product with FP16 result: optional FP16 row [N] added before the rounding, or NULL
   void* colsum;            // GELU_GRAD: optional FP32 [ceil(M / 32)][N] that receives the column sums of the FP16 result per
                            // 32-row block (every element written), or NULL
+  void* keep_scale;        // gated block: scales of Z's 8-bit blocks
+  void* gate_h;            // gated block: H [M][f]
+  float gate_alpha;        // gated block, backward: H's factor (epi_scale, skip_scale: those of dZ's halves)
   void* table;             // table area of the workspace (us_device.h), or NULL: arithmetic epilogue
   bool tables_ready;       // the table area is already filled for this epi_scale
   size_t workspace_bytes;
@@ -144,6 +164,11 @@ long gemm_k_per_split(long K, int splits);
 size_t gemm_workspace_bytes(long M, long N, long K);
 
 hipError_t launch_gemm(const GemmProblem& p, hipStream_t stream);
+// The two products of the gated block that have epilogues of their own (us_gemm_gate.h).  Forward: A = X [M,K], B = Wgu [K,N = 2f], C = Z or
+// NULL; backward: A = G [M,K], B = Wd [N = f,K], Zpre = Z, C or aux8 = dZ; ldc = 2f, act = the gate, keep8: Z in 8-bit blocks.
+bool gemm_gate_offsets_fit(const GemmProblem& p);
+hipError_t gemm_gate_fwd(const GemmProblem& p, bool keep8, hipStream_t stream);
+hipError_t gemm_gate_grad(const GemmProblem& p, bool keep8, hipStream_t stream);
 // Two batches of equally shaped FP16 products with both operands K-strided (attention's dV and dK) in one launch.
 hipError_t gemm_tn_f16_two_batches(const GemmProblem& p, const GemmProblem& q, hipStream_t stream);
 

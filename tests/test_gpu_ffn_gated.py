@@ -1,0 +1,309 @@
+"""The gated feed-forward block against its definition in 64 bits, stage by stage on the tensors that the GPU stored.
+
+Products with FP16 results (Z, Y, dX, dWgu, dWd) go by the matmul metric of the other tests (gpu_util.assert_close).  Codes: an E4M3 / E5M2 code is the
+nearest value to a number that may be off by `slack`, so it is within half a step (2^-4, 2^-3 of the value; half of the least step among
+subnormals) plus slack; an 8-bit block's code within half a step plus slack, and its step is the definition's but where the block's largest
+magnitude lies within slack of a border.  slack: what the matrix core's sums are off (parity.py: FP8 operands 2e-4 of a unit; FP16 2^-20 sqrt(K)
+of a unit, FP32 sums in any order) times the derivative towards it, at most |f| + |f'||zu| <= 1.13 |zu| + |zg| + 1, times the factor.
+
+The metric's absolute part for FP8 operands, 2e-4 of a unit, was measured on normal operands.  H and dZ are products of two and three normal
+numbers, with tails to match, and the matrix core's adder keeps about 14 bits below the largest product of a group: where a group
+holds a product P, its sum may be off by 2^-13 P, and all groups together by 2^-12 of the sum of all magnitudes, which is therefore what products with
+such an operand are allowed per element (as the range-stress products are).  That bound is wide, so their error's 2-norm is held as well: rounding to
+FP16 is off by at most 2^-11 with a uniform distribution, 2^-11 / sqrt(3) = 2.82e-4 of the values' rms, the adder by 1.4e-5 rms of a unit on normal
+operands and at most five times that on these, and (2.82e-4^2 + 7e-5^2)^1/2 < 3e-4.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import gated_ref as R
+import paper_2303_11257_amd as us
+from gpu_util import DEV, assert_close, ptr, stream
+
+pytestmark = pytest.mark.gpu
+
+
+class Block:
+    """Operands and buffers of one block; outputs have a guard row behind them."""
+
+    def __init__(self, T, d, f, fp8, keep8, gate, seed=1, sigma=1.0):
+        g = torch.Generator().manual_seed(seed)
+        self.T, self.d, self.f, self.fp8, self.keep8, self.gate = T, d, f, fp8, keep8, gate
+        self.mode = (us.FFN_FP8 if fp8 else 0) | (us.FFN_KEEP8 if keep8 else 0)
+        rnd = lambda *s: (torch.randn(s, generator=g) * sigma).half()      # noqa: E731
+        self.X, self.Wgu, self.Wd, self.G = rnd(T, d), rnd(d, 2 * f), rnd(f, d), rnd(T, d)
+        if fp8:
+            self.X, self.Wgu, self.Wd = (x.float().clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8) for x in (self.X, self.Wgu, self.Wd))
+            self.G = self.G.float().clamp(-57344, 57344).to(torch.float8_e5m2).view(torch.uint8)
+        self.g = {k: getattr(self, k).to(DEV) for k in ("X", "Wgu", "Wd", "G")}
+        el = torch.uint8 if fp8 else torch.float16
+        new = lambda r, c, t: torch.full((r + 1, c), 7, dtype=t, device=DEV)      # noqa: E731
+        self.Z = new(T, 2 * f, torch.int8 if keep8 else torch.float16)
+        self.Zs = new(T, 2 * us.keep8_blocks(f), torch.uint8) if keep8 else None
+        self.H, self.Y, self.dZ, self.dX = new(T, f, el), new(T, d, torch.float16), new(T, 2 * f, el), new(T, d, torch.float16)
+        self.dWgu, self.dWd = new(d, 2 * f, torch.float16), new(f, d, torch.float16)
+        self.wsb = us.ffn_gated_workspace_bytes(T, d, f, self.mode)
+        self.ws = torch.full((max(16, self.wsb),), 0xff, dtype=torch.uint8, device=DEV)
+
+    def forward(self, st=None, keep=True, ws=True, **kw):
+        us.ffn_gated_fwd(ptr(self.g["X"]), ptr(self.g["Wgu"]), ptr(self.g["Wd"]), ptr(self.Z) if keep else None, ptr(self.Zs), ptr(self.H), ptr(self.Y), self.T, self.d,
+                         self.f, self.gate, self.mode, ptr(self.ws) if ws else None, self.wsb if ws else 0, stream() if st is None else st, **kw)
+        return self
+
+    def backward(self, st=None, skip=(), **kw):
+        us.ffn_gated_bwd(ptr(self.g["X"]), ptr(self.g["Wgu"]), ptr(self.g["Wd"]), ptr(self.Z), ptr(self.Zs), ptr(self.H), ptr(self.g["G"]), ptr(self.dZ),
+                         *(None if n in skip else ptr(getattr(self, n)) for n in ("dX", "dWgu", "dWd")), self.T, self.d, self.f, self.gate, self.mode, ptr(self.ws),
+                         self.wsb, stream() if st is None else st, **kw)
+        return self
+
+    def outputs(self):
+        torch.cuda.synchronize()
+        return {n: getattr(self, n).cpu() for n in ("Z", "Zs", "H", "Y", "dZ", "dX", "dWgu", "dWd") if getattr(self, n) is not None}
+
+
+def operand(x, e5m2=False):
+    return R.fp8_values(x, e5m2) if x.dtype == torch.uint8 else x.double()
+
+
+def product_close(b, got, A, B, factor, what):
+    want = A @ B * factor
+    if not b.fp8:
+        assert_close(got.numpy(), want.numpy(), what, scale=max(1.0, float(want.square().mean().sqrt())))
+        return
+    scale = float(want.square().mean().sqrt())
+    assert_close(got.numpy(), want.numpy(), what, fp8=True, scale=scale, allow=(A.abs() @ B.abs() * (factor * 2.0 ** -12)).numpy())
+    assert float((got.double() - want).square().mean().sqrt()) <= 3e-4 * scale + 2.0 ** -25, what
+
+
+def slack_of(b, zg, zu, factor):
+    unit = (2e-4 if b.fp8 else 2.0 ** -20 * math.sqrt(b.d))
+    return factor * unit * (2 + zg.abs() + 1.2 * zu.abs())
+
+
+def near_codes(codes, e5m2, want, slack, what):
+    v = R.fp8_values(codes, e5m2)
+    least, rel, top = (2.0 ** -17, 2.0 ** -3, 57344.0) if e5m2 else (2.0 ** -10, 2.0 ** -4, 448.0)
+    w = want.clamp(-top, top)
+    bad = (v - w).abs() > torch.clamp(w.abs() * rel, min=least) + slack
+    assert not bad.any(), (what, int(bad.sum()), float((v - w).abs()[bad].max()))
+
+
+def kept(b, out):
+    """The values that the backward pass reads, [T, f] each."""
+    z = out["Z"][: b.T]
+    if not b.keep8:
+        return z[:, : b.f].double(), z[:, b.f:].double()
+    nb = us.keep8_blocks(b.f)
+    s = out["Zs"][: b.T].numpy()
+    return tuple(torch.from_numpy(R.keep8_values(z[:, i * b.f: (i + 1) * b.f].numpy(), s[:, i * nb: (i + 1) * nb])) for i in (0, 1))
+
+
+def check_forward(b, out, alpha=None):
+    gate = R.GATES[b.gate]
+    a = us.gate_scales(b.gate)[0] if alpha is None else alpha
+    X, Wgu, Wd = (operand(getattr(b, n)) for n in ("X", "Wgu", "Wd"))
+    Z = X @ Wgu / math.sqrt(b.d)
+    zg, zu = Z[:, : b.f], Z[:, b.f:]
+    if not b.keep8:
+        assert_close(out["Z"][: b.T].numpy(), Z.numpy(), "Z", fp8=b.fp8)
+    else:
+        nb = us.keep8_blocks(b.f)
+        unit = slack_of(b, torch.zeros(()), torch.zeros(()), 1.0).item()
+        for i, z in enumerate((zg, zu)):
+            codes, scales = out["Z"][: b.T, i * b.f: (i + 1) * b.f].numpy(), out["Zs"][: b.T, i * nb: (i + 1) * nb].numpy()
+            lo, hi = R.keep8(z.numpy() * (1 - 1e-6) - np.sign(z.numpy()) * unit)[1], R.keep8(z.numpy() * (1 + 1e-6) + np.sign(z.numpy()) * unit)[1]
+            assert ((scales >= lo) & (scales <= hi)).all()
+            step = np.repeat(2.0 ** (scales.astype(np.float64) - 127), 32, axis=1)[:, : b.f]
+            assert (np.abs(codes * step - z.numpy()) <= step / 2 + unit * (1 + np.abs(z.numpy()))).all()
+    H = a * R.gate_value(gate, zg) * zu
+    if b.fp8:
+        near_codes(out["H"][: b.T], False, H, slack_of(b, zg, zu, a), "H")
+    else:
+        d = (out["H"][: b.T].double() - H).abs()
+        assert (d <= 2.0 ** -11 * H.abs() + 2.0 ** -25 + 1e-5 * H.abs() + slack_of(b, zg, zu, a)).all()
+    product_close(b, out["Y"][: b.T], operand(out["H"][: b.T]), Wd, b.f ** -0.5, "Y")
+    for n in ("Z", "Zs", "H", "Y"):
+        if n in out:
+            assert (out[n][b.T].float() == 7).all(), n
+
+
+def check_backward(b, out, alpha=None, beta_gate=None, beta_up=None):
+    gate = R.GATES[b.gate]
+    da, db = us.gate_scales(b.gate)
+    a, bg, bu = (d if x is None else x for x, d in ((alpha, da), (beta_gate, db), (beta_up, da)))
+    X, Wgu, Wd, G = operand(b.X), operand(b.Wgu), operand(b.Wd), operand(b.G, True)
+    zg, zu = kept(b, out)
+    dH = G @ Wd.t() / math.sqrt(b.d)
+    F, S = R.gate_value(gate, zg), R.gate_slope(gate, zg)
+    want = torch.cat([bg * S * zu * dH, bu * F * dH], 1)
+    unit = 2e-4 if b.fp8 else 2.0 ** -20 * math.sqrt(b.d)
+    # dH's own error, and the gate functions' 2e-5 (the fitted tail of gelu 4e-6 of the probability, exponentials and reciprocals 2^-22)
+    room = unit * torch.cat([bg * (S * zu).abs(), bu * F.abs()], 1) + 2e-5 * torch.cat([bg * (zu * dH).abs(), bu * (1 + zg.abs()) * dH.abs()], 1)
+    if b.fp8:
+        near_codes(out["dZ"][: b.T], True, want, room, "dZ")
+    else:
+        assert ((out["dZ"][: b.T].double() - want).abs() <= 2.0 ** -11 * want.abs() + 2.0 ** -25 + room).all()
+    if b.keep8:
+        H = a * F * zu
+        if b.fp8:
+            near_codes(out["H"][: b.T], False, H, 2e-5 * a * (1 + zg.abs()) * zu.abs(), "H again")
+        else:
+            assert ((out["H"][: b.T].double() - H).abs() <= 2.0 ** -11 * H.abs() + 2.0 ** -25 + 2e-5 * a * (1 + zg.abs()) * zu.abs()).all()
+    dZ, H = operand(out["dZ"][: b.T], True), operand(out["H"][: b.T])
+    product_close(b, out["dX"][: b.T], dZ, Wgu.t(), (2 * b.f) ** -0.5, "dX")
+    product_close(b, out["dWgu"][: b.d], X.t(), dZ, b.T ** -0.5, "dWgu")
+    product_close(b, out["dWd"][: b.f], H.t(), G, b.T ** -0.5, "dWd")
+    for n, r in (("dZ", b.T), ("dX", b.T), ("dWgu", b.d), ("dWd", b.f), ("H", b.T)):
+        assert (out[n][r].float() == 7).all(), n
+
+
+# one token, a few, odd numbers; widths that end inside a block of 32, a tile's half and a tile; all kernels' tiles
+SHAPES = [(1, 16, 16), (1, 256, 688), (5, 48, 32), (33, 64, 80), (64, 528, 144), (65, 512, 2064), (130, 256, 272), (600, 512, 1040), (1999, 272, 528), (2048, 128, 2064), (1300, 64, 4112)]
+
+
+@pytest.mark.parametrize("keep8", [False, True])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,d,f", SHAPES)
+def test_forward_and_backward(T, d, f, fp8, keep8):
+    b = Block(T, d, f, fp8, keep8, us.GATE_SILU, seed=T + f)
+    b.forward()
+    first = b.outputs()
+    check_forward(b, first)
+    if keep8:
+        b.H.view(torch.uint8)[: b.T].fill_(0x3c)             # the forward call's H is not read again
+    b.backward()
+    out = b.outputs()
+    assert torch.equal(out["Z"], first["Z"])
+    check_backward(b, out)
+
+
+@pytest.mark.parametrize("keep8", [False, True])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("gate", range(4))
+@pytest.mark.parametrize("T,d,f", [(40, 96, 208), (700, 96, 1296)])
+def test_gates_and_factors(T, d, f, gate, fp8, keep8):
+    b = Block(T, d, f, fp8, keep8, gate, seed=gate)
+    b.forward().backward()
+    out = b.outputs()
+    if not keep8:
+        check_forward(b, out)
+    check_backward(b, out)
+    kw = dict(alpha=1.25, beta_gate=0.75, beta_up=0.5)
+    b.forward(alpha=1.25)
+    check_forward(b, b.outputs(), alpha=1.25)
+    b.backward(**kw)
+    check_backward(b, b.outputs(), **kw)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,d,f", [(1, 512, 1376), (16, 256, 688), (300, 256, 1040)])
+def test_serving_keeps_nothing_and_answers_the_same(T, d, f, fp8):
+    b = Block(T, d, f, fp8, False, us.GATE_GELU)
+    y = b.forward().outputs()
+    b.Y.fill_(7), b.H.fill_(7), b.Z.fill_(3)
+    z = b.forward(keep=False, ws=False).outputs()
+    assert (z["Z"] == 3).all()
+    assert torch.equal(y["H"], z["H"]) and torch.equal(y["Y"], z["Y"])
+    c = Block(T, d, f, fp8, True, us.GATE_GELU)              # what is kept does not change the answer either
+    k = c.forward().outputs()
+    assert torch.equal(y["H"], k["H"]) and torch.equal(y["Y"], k["Y"])
+
+
+def test_single_gradients_and_none_of_no_tokens():
+    b = Block(130, 64, 96, False, True, us.GATE_SILU)
+    full = b.forward().backward().outputs()
+    for n in ("dX", "dWgu", "dWd"):
+        c = Block(130, 64, 96, False, True, us.GATE_SILU)
+        o = c.forward().backward(skip=[n]).outputs()
+        assert (o[n] == 7).all()
+        for other in {"dX", "dWgu", "dWd"} - {n}:
+            assert_close(o[other][:-1].numpy(), full[other][:-1].double().numpy(), other)
+    e = Block(0, 64, 96, True, False, us.GATE_SILU)
+    o = e.forward().backward().outputs()
+    assert (o["dWgu"][:64] == 0).all() and (o["dWd"][:96] == 0).all() and (o["dX"] == 7).all()
+
+
+@pytest.mark.parametrize("T", [3, 700])
+def test_infinities_and_nan_stay_in_their_rows(T):
+    """A NaN and an infinity in X reach their own rows of Z, H, Y and dX only; 8-bit blocks hold NaN and clip infinities."""
+    for keep8 in (False, True):
+        b = Block(T, 64, 2080 if T > 3 else 96, False, keep8, us.GATE_SILU)
+        clean = b.forward().backward().outputs()
+        b.g["X"][1, 5] = float("nan")
+        b.g["X"][2, 9] = float("inf")
+        dirty = b.forward().backward().outputs()
+        others = [r for r in range(T) if r not in (1, 2)]
+        for n in ("Z", "H", "Y", "dZ", "dX"):
+            assert torch.equal(clean[n][others], dirty[n][others]), n
+        assert torch.isnan(dirty["Y"][1]).all() and torch.isnan(dirty["dX"][1]).all()
+        if keep8:
+            assert (dirty["Z"][1] == -128).all() and (dirty["Z"][2].abs() == 127).all() and (dirty["Zs"][2] == 136).all() and (dirty["Zs"][1] == 103).all()
+        else:
+            assert torch.isnan(dirty["Z"][1]).all() and torch.isinf(dirty["Z"][2]).all()
+
+
+def test_gradients_against_differences():
+    """With one factor for both halves of dZ the gradients are those of <Y, G> up to known factors: dX (2f)^1/2 (f/d)^-1/2 ... all products' factors
+    divided out.  Central difference in 64 bits along a direction v, step 2^-8: its error, h^2 / 6 times a third derivative of order one per
+    element, is below 2^-17 of the sums' size; the FP16 roundings of Z, dZ and dX are 2^-11 each per element with independent signs: below
+    3 * 2^-10 of <|dX|, |v|> / sqrt(n), times a generous 8."""
+    T, d, f = 24, 48, 64
+    b = Block(T, d, f, False, False, us.GATE_SILU, seed=3)
+    a = us.gate_scales(us.GATE_SILU)[0]
+    b.forward().backward(alpha=a, beta_gate=a, beta_up=a)
+    out = b.outputs()
+    X, Wgu, Wd, G = (getattr(b, n).double() for n in ("X", "Wgu", "Wd", "G"))
+
+    def value(X, Wgu, Wd):
+        Z = X @ Wgu / math.sqrt(d)
+        return float((((a * R.gate_value("silu", Z[:, :f]) * Z[:, f:]) @ Wd / math.sqrt(f)) * G).sum())
+
+    # true gradient / stored one: dH f^-1/2 instead of d^-1/2; dX d^-1/2 instead of (2f)^-1/2; weights d^-1/2 (f^-1/2) instead of T^-1/2
+    hs = math.sqrt(d / f)
+    gen = torch.Generator().manual_seed(4)
+    for name, at, factor in (("dX", 0, hs * math.sqrt(2 * f / d)), ("dWgu", 1, hs * math.sqrt(T / d)), ("dWd", 2, math.sqrt(T / f))):
+        g = out[name][:-1].double() * factor
+        v = torch.randn(g.shape, generator=gen, dtype=torch.float64)
+        h, p = 2.0 ** -8, [X, Wgu, Wd]
+        p[at] = p[at] + h * v
+        up = value(*p)
+        p[at] = p[at] - 2 * h * v
+        diff = (up - value(*p)) / (2 * h)
+        size = float((g.abs() * v.abs()).sum())
+        assert abs(diff - float((g * v).sum())) <= size * (24 * 2.0 ** -10 / math.sqrt(v.numel()) + 2.0 ** -14), name
+
+
+def test_captured_replayed_and_two_streams():
+    blocks = [Block(70, 128, 272, fp8, True, us.GATE_SILU, seed=s) for s, fp8 in ((1, False), (2, True))]
+    eager = [b.forward().backward().outputs() for b in blocks]
+    graphs, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for b, st in zip(blocks, streams):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            now = torch.cuda.current_stream().cuda_stream
+            b.forward(now).backward(now)
+        graphs.append(graph)
+    for _ in range(4):
+        for b in blocks:
+            for n in ("Z", "H", "Y", "dZ", "dX"):
+                getattr(b, n)[: b.T].zero_()
+        torch.cuda.synchronize()
+        for graph, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                graph.replay()
+        torch.cuda.synchronize()
+        for b, e in zip(blocks, eager):
+            o = b.outputs()
+            assert all(torch.equal(o[n], e[n]) for n in e)
+
+
+def test_unit_variance():
+    """Unit-normal operands: the tensors that the factors are for have unit variance (5 %, the bound of the other layers' tests)."""
+    b = Block(2048, 256, 704, False, False, us.GATE_SILU)
+    out = b.forward().backward().outputs()
+    for n in ("Z", "H", "Y", "dX", "dWgu", "dWd"):
+        assert abs(float(out[n][:-1].double().square().mean()) - 1) < 0.05, n
+    assert abs(float(out["dZ"][:-1].double().square().mean()) - 1) < 0.05
