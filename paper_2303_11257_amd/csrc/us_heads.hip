@@ -101,17 +101,35 @@ struct Lane {
   }
 };
 
-__device__ __forceinline__ void load16(float (&v)[16], const _Float16* p, const Lane& l) {
-  v8h a = {0, 0, 0, 0, 0, 0, 0, 0}, b = a;
-  if (l.on) {
-    a = *reinterpret_cast<const v8h*>(p + l.a);
-    b = *reinterpret_cast<const v8h*>(p + l.b);
+// A lane's values as they lie in memory.
+struct Raw {
+  v8h a, b;
+  __device__ __forceinline__ void load(const _Float16* p, const Lane& l) {
+    a = b = v8h{0, 0, 0, 0, 0, 0, 0, 0};
+    if (l.on) {
+      a = *reinterpret_cast<const v8h*>(p + l.a);
+      b = *reinterpret_cast<const v8h*>(p + l.b);
+    }
   }
+  __device__ __forceinline__ void get(float (&v)[16]) const {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    v[k] = (float)a[k];
-    v[k + 8] = (float)b[k];
+    for (int k = 0; k < 8; ++k) {
+      v[k] = (float)a[k];
+      v[k + 8] = (float)b[k];
+    }
   }
+  __device__ __forceinline__ void add_to(float (&v)[16]) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      v[k] += (float)a[k];
+      v[k + 8] += (float)b[k];
+    }
+  }
+};
+__device__ __forceinline__ void load16(float (&v)[16], const _Float16* p, const Lane& l) {
+  Raw r;
+  r.load(p, l);
+  r.get(v);
 }
 __device__ __forceinline__ void store16(_Float16* p, const float (&v)[16], const Lane& l) {
   v8h a, b;
@@ -169,36 +187,47 @@ __global__ void __launch_bounds__(kThreads) heads_fwd_kernel(HeadsArgs a, _Float
 }
 
 // Partial weights' gradients: one FP32 row [2][dh] (wq, wk) per workgroup in `partial`, added by the next kernel in order.
-template <int G, bool HALVES>
+// WPT waves work on a token: one where there are tokens for every wave (a token's query, key and value heads then come round after round, and no wave
+// waits for another's share), all four where there are few.
+template <int G, bool HALVES, int WPT>
 __global__ void __launch_bounds__(kThreads) heads_bwd_kernel(HeadsArgs a, const _Float16* __restrict__ dQ, const _Float16* __restrict__ dK,
                                                              const _Float16* __restrict__ dV, _Float16* __restrict__ dx, long ld_dx,
                                                              float rep_scale, float* __restrict__ partial) {
   __shared__ float sums[kThreads / G][16 * G];
+  constexpr int GROUPS = 64 / G * WPT, TOKENS = kThreads / 64 / WPT;            // lane groups on a token, tokens of a workgroup
   const Lane lane = Lane::of<HALVES>((int)threadIdx.x % G, a.dh, a.rot);
-  const int group = (int)threadIdx.x / G;
+  const int group = (int)threadIdx.x / G % GROUPS;
   const float per = 1.0f / (float)a.dh;
   LaneAngles ang;
   ang.init(a.freq, lane.first, lane.rotated);
   float sq[16], sk[16];
 #pragma unroll
   for (int k = 0; k < 16; ++k) sq[k] = sk[k] = 0.0f;
-  for (long t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+  for (long t = (long)blockIdx.x * TOKENS + (int)threadIdx.x / (64 * WPT); t < a.tokens; t += (long)gridDim.x * TOKENS) {
     const long b = t / a.s, i = t - b * a.s;
     ang.at(a.pos ? a.pos[t] : (int)i, lane.rotated);
     const _Float16* row = a.x + t * a.ld;
     _Float16* drow = dx + t * ld_dx;
-    for (int slot = group; slot < a.h + 2 * a.kv; slot += kThreads / G) {
+    const long head_step = (long)a.s * a.dh;
+    for (int slot = group; slot < a.h + 2 * a.kv; slot += GROUPS) {
       const bool is_v = slot >= a.h + a.kv, is_q = slot < a.h;
       const int rep = is_q ? 1 : a.rep;
       const _Float16* dy = is_q ? dQ : is_v ? dV : dK;
       const int head = is_q ? slot : (is_v ? slot - a.h - a.kv : slot - a.h) * a.rep;
+      dy += ((b * a.h + head) * a.s + i) * a.dh;
+      // everything that is read first, the sharing heads' gradients four at a time: one chain of memory latencies per round
+      Raw x, y[4];
+      if (!is_v) x.load(row + (long)slot * a.dh, lane);
       float g[16];
-      load16(g, dy + ((b * a.h + head) * a.s + i) * a.dh, lane);
-      for (int r = 1; r < rep; ++r) {
-        float o[16];
-        load16(o, dy + ((b * a.h + head + r) * a.s + i) * a.dh, lane);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) g[k] += o[k];
+      for (int k = 0; k < 16; ++k) g[k] = 0.0f;
+      for (int r = 0; r < rep; r += 4) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (r + q < rep) y[q].load(dy + (r + q) * head_step, lane);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (r + q < rep) y[q].add_to(g);
       }
       if (rep > 1) {
 #pragma unroll
@@ -206,7 +235,7 @@ __global__ void __launch_bounds__(kThreads) heads_bwd_kernel(HeadsArgs a, const 
       }
       if (!is_v) {
         float v[16], w[16];
-        load16(v, row + (long)slot * a.dh, lane);
+        x.get(v);
         weights16(w, is_q ? a.wq : a.wk, lane);
         turn<HALVES, true>(g, ang, lane.rotated);
         float ss = 0.0f;
@@ -231,14 +260,15 @@ __global__ void __launch_bounds__(kThreads) heads_bwd_kernel(HeadsArgs a, const 
     }
   }
   // the workgroup's sums, group after group
+  const int slice = (int)threadIdx.x / G;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     __syncthreads();
     if (lane.on) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        sums[group][lane.a + k] = which ? sk[k] : sq[k];
-        sums[group][lane.b + k] = which ? sk[k + 8] : sq[k + 8];
+        sums[slice][lane.a + k] = which ? sk[k] : sq[k];
+        sums[slice][lane.b + k] = which ? sk[k + 8] : sq[k + 8];
       }
     }
     __syncthreads();
@@ -256,7 +286,15 @@ __global__ void __launch_bounds__(kThreads) heads_dw_kernel(const float* __restr
   __shared__ float sums[16][16];
   const int c = (int)threadIdx.x % 16, part = (int)threadIdx.x / 16, col = (int)blockIdx.x * 16 + c;      // of 2 * dh, whole workgroups
   float s = 0.0f;
-  for (int r = part; r < rows; r += 16) s += partial[(long)r * 2 * dh + col];
+  int r = part;
+  for (; r + 7 * 16 < rows; r += 8 * 16) {             // eight reads in flight
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = partial[(long)(r + k * 16) * 2 * dh + col];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += v[k];
+  }
+  for (; r < rows; r += 16) s += partial[(long)r * 2 * dh + col];
   sums[part][c] = s;
   __syncthreads();
   if (part == 0) {
@@ -268,10 +306,13 @@ __global__ void __launch_bounds__(kThreads) heads_dw_kernel(const float* __restr
   }
 }
 
+// Workgroups of the backward kernel: four per CU, which is what its registers allow, or one per token.
 long bwd_groups(long tokens) {
   const long most = 4 * (long)device_info().cus;
   return tokens < most ? tokens : most;
 }
+// Tokens for every wave of those workgroups?
+bool wave_per_token(long tokens) { return tokens >= 16 * (long)device_info().cus; }
 
 // f(integral_constant<int, G>, bool_constant<HALVES>), G: the power of two of lanes that holds dh / 16
 template <class F>
@@ -312,8 +353,12 @@ hipError_t launch_heads_bwd(const HeadsCall& c, const void* dQ, const void* dK, 
   float* partial = (float*)workspace;
   const float rep_scale = (float)(1.0 / __builtin_sqrt((double)(c.heads / c.kv_heads)));
   const hipError_t e = with_shape(c.dh, c.pairs, [&](auto g, auto halves) {
-    heads_bwd_kernel<decltype(g)::value, decltype(halves)::value><<<(unsigned)rows, kThreads, 0, st>>>(
-        heads_args(c), (const _Float16*)dQ, (const _Float16*)dK, (const _Float16*)dV, (_Float16*)dQKV, ld_dx, rep_scale, partial);
+    auto go = [&](auto wpt) {
+      heads_bwd_kernel<decltype(g)::value, decltype(halves)::value, decltype(wpt)::value><<<(unsigned)rows, kThreads, 0, st>>>(
+          heads_args(c), (const _Float16*)dQ, (const _Float16*)dK, (const _Float16*)dV, (_Float16*)dQKV, ld_dx, rep_scale, partial);
+    };
+    if (wave_per_token(c.batch * c.s)) go(std::integral_constant<int, 1>{});
+    else go(std::integral_constant<int, 4>{});
   });
   if (e != hipSuccess || (!dwq && !dwk)) return e;
   heads_dw_kernel<<<(unsigned)(2 * c.dh / 16), kThreads, 0, st>>>(partial, (_Float16*)dwq, (_Float16*)dwk, (int)rows, (int)c.dh, beta_wq, beta_wk);
