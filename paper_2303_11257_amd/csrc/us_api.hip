@@ -713,10 +713,14 @@ us_status us_gate_scales(us_gate gate, float* alpha, float* beta) {
 }
 
 size_t us_ffn_gated_workspace_bytes(long T, long d, long f, int mode) {
-  (void)mode;
   if (T < 1 || d < 1 || f < 1) return 0;
-  const size_t a = us_workspace_bytes(T, f, d), b = us_workspace_bytes(T, d, 2 * f);      // dWd and dWgu
-  return a > b ? a : b;
+  const bool fp8 = (mode & US_FFN_FP8) != 0;
+  if (d > US_FFN_GATED_MAX || f > US_FFN_GATED_MAX) return 0;               // refused sizes
+  size_t n = us_workspace_bytes(T, f, d);                                   // dWd
+  auto at_least = [&](size_t v) { n = v > n ? v : n; };
+  at_least(us_workspace_bytes(T, d, 2 * f));                               // dWgu
+  at_least(gemm_rows_workspace_bytes(T, d, f, fp8));                        // few tokens: both projections' slices, one after the other
+  return n;
 }
 
 // What both directions check first.  The rows of Z and Wgu bound f: the kernels address a tile with 32-bit offsets.
@@ -736,7 +740,6 @@ us_status us_ffn_gated_fwd(const void* X, const void* Wgu, const void* Wd, void*
   if (!X || !Wgu || !Wd || !H || !Y || (keep8 && (!Z || !Zs))) return US_ERR_NULL;
   if (!aligned16(X) || !aligned16(Wgu) || !aligned16(Wd) || !aligned16(Z) || !aligned16(Zs) || !aligned16(H) || !aligned16(Y) || !aligned16(workspace))
     return US_ERR_ALIGN;
-  (void)workspace_bytes;
   const us_dtype op = fp8 ? US_E4M3 : US_F16;
   GemmProblem p{};
   p.A = X; p.B = Wgu; p.C = Z;
@@ -750,6 +753,16 @@ us_status us_ffn_gated_fwd(const void* X, const void* Wgu, const void* Wd, void*
   p.keep_scale = Zs;
   p.gate_h = H;
   if (!gemm_gate_offsets_fit(p)) return US_ERR_SHAPE;
+  // few tokens: both projections as streams of their weights, if the workspace holds their slices
+  GemmProblem q{};
+  q.A = H; q.B = Wd; q.C = Y;
+  q.M = T; q.N = d; q.K = f;
+  q.lda = f; q.ldb = d; q.ldc = d;
+  q.a_kc = true; q.b_kc = false;
+  q.a_dt = op; q.b_dt = op; q.c_dt = US_F16;
+  q.scale = (float)(1.0 / sqrt((double)f));
+  if (workspace && gemm_rows_take(T, d, f, fp8) && workspace_bytes >= gemm_rows_workspace_bytes(T, d, f, fp8))
+    return from_hip(gemm_rows_ffn(p, q, keep8, workspace, as_stream(stream)));
   if (us_status s = from_hip(gemm_gate_fwd(p, keep8, as_stream(stream))); s != US_OK) return s;
   return linear_fwd_impl(H, Wd, nullptr, Y, T, f, d, op, op, US_F16, 0.0f, US_EPI_NONE, 0.0f, nullptr, nullptr, nullptr, 0, stream, true, true);
 }

@@ -199,17 +199,31 @@ def test_gates_and_factors(T, d, f, gate, fp8, keep8):
 
 
 @pytest.mark.parametrize("fp8", [False, True])
-@pytest.mark.parametrize("T,d,f", [(1, 512, 1376), (16, 256, 688), (300, 256, 1040)])
+@pytest.mark.parametrize("T,d,f", [(1, 1024, 4400), (16, 256, 688), (300, 256, 1040)])
 def test_serving_keeps_nothing_and_answers_the_same(T, d, f, fp8):
     b = Block(T, d, f, fp8, False, us.GATE_GELU)
     y = b.forward().outputs()
     b.Y.fill_(7), b.H.fill_(7), b.Z.fill_(3)
-    z = b.forward(keep=False, ws=False).outputs()
+    z = b.forward(keep=False).outputs()
     assert (z["Z"] == 3).all()
     assert torch.equal(y["H"], z["H"]) and torch.equal(y["Y"], z["Y"])
     c = Block(T, d, f, fp8, True, us.GATE_GELU)              # what is kept does not change the answer either
     k = c.forward().outputs()
     assert torch.equal(y["H"], k["H"]) and torch.equal(y["Y"], k["Y"])
+    w = Block(T, d, f, fp8, False, us.GATE_GELU)             # without a workspace the sums may be taken in another order
+    check_forward(w, w.forward(ws=False).outputs())
+
+
+# (tokens, d, f): the streams of weights, every row count they take and the next; slices of several steps, the last one shorter; f and d that end inside a strip
+@pytest.mark.parametrize("fp8,T", [(False, t) for t in (1, 2, 3, 4, 5, 8, 9)] + [(True, t) for t in (1, 2, 3, 4, 5)])
+def test_a_few_rows(T, fp8):
+    for d, f, keep8 in (((2064, 10896, False), (11024, 2032, True)) if fp8 else ((1040, 4400, False), (4112, 1040, True))):
+        b = Block(T, d, f, fp8, keep8, us.GATE_SILU, seed=T * d)
+        check_forward(b, b.forward().outputs())
+        assert ("stream" in us.last_launch()) == (T <= (4 if fp8 else 8))
+        w = Block(T, d, f, fp8, keep8, us.GATE_SILU, seed=T * d)      # without a workspace the sums are taken in another order
+        check_forward(w, w.forward(ws=False).outputs())
+        assert "stream" not in us.last_launch()
 
 
 def test_single_gradients_and_none_of_no_tokens():
