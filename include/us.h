@@ -468,7 +468,8 @@ size_t us_ffn_gated_workspace_bytes(long T, long d, long f, int mode);
  * 32 (the last one may be shorter) share a step 2^e, the smallest power of two from 2^-24 to 2^9 whose 127.5 steps no magnitude of the
  * block reaches; a value is held as the whole number of steps nearest to it (ties to even).  Magnitudes from 127.5 * 2^9 on, infinities
  * among them, are held as 127 steps of their sign; NaN as -128, and does not count for e.
- *   store: X [rows,n] FP16, rows `ld` elements apart -> codes int8 [rows,n], scales uint8 [rows, us_keep8_blocks(n)] holding e + 127
+ *   store: X [rows,n] FP16, rows `ld` elements apart -> codes int8 [rows,n], scales uint8 [rows, us_keep8_blocks(n)] holding e + 127, plus
+ *          64 for a block with a NaN
  *   load:  the values that the codes stand for, which FP16 holds exactly; elements of X beyond column n of a row are left as they were
  * n a multiple of 16, ld >= n a multiple of 8; rows is free; all pointers 16-byte aligned.  The error of a value is at most half a
  * step, below 2^-7 of the block's largest magnitude.  us_keep8_blocks(n) = ceil(n / 32).

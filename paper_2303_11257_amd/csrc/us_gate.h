@@ -18,8 +18,8 @@ struct GateTerms {
   float f, slope;      // f(z) and f'(z)
 };
 // gate: 0 silu, 1 gelu, 2 relu, 3 sigmoid (us_gate).  One exponential and one reciprocal for silu and sigmoid: p = 1 / (1 + 2^(-z log2 e)) keeps
-// its relative accuracy on both sides; 1 - p loses it only where it is small next to the terms it is added to.  The exponent stops at 126, so
-// that p stays a normal number (f and f' are below FP16's range there).  A NaN gives NaN.
+// its relative accuracy on both sides; 1 - p loses it only where it is small next to the terms it is added to.  From z = -88 on the exponential
+// is infinite and p zero, as f and f' are in every result type.  (sigmoid' needs p e, so its exponent stops at 126.)  A NaN gives NaN.
 template <int GATE>
 __device__ __forceinline__ GateTerms gate_terms(float z) {
   if constexpr (GATE == 1) {
@@ -28,8 +28,9 @@ __device__ __forceinline__ GateTerms gate_terms(float z) {
   } else if constexpr (GATE == 2) {
     return {z <= 0.0f ? 0.0f : z, z > 0.0f ? 1.0f : 0.0f};
   } else {
-    const float x = -1.4426950408889634f * z;
-    const float e = __builtin_amdgcn_exp2f(x > 126.0f ? 126.0f : x);
+    float x = -1.4426950408889634f * z;
+    if constexpr (GATE == 3) x = x > 126.0f ? 126.0f : x;
+    const float e = __builtin_amdgcn_exp2f(x);
     const float p = __builtin_amdgcn_rcpf(1.0f + e);
     if constexpr (GATE == 3) return {p, p * (p * e)};
     const float f = z * p;
@@ -49,10 +50,11 @@ __device__ __forceinline__ void with_gate(int gate, F f) {
 // ---- 8-bit blocks ----------------------------------------------------------------------------------------------------------
 // 32 values x share a step 2^e, the smallest power of two from 2^-24 to 2^9 whose 127.5 steps none of their magnitudes reaches; the code of
 // a value is round(x / 2^e), at most 127 steps (beyond 127.5 * 2^9, infinities among them, values are clipped), -128 for NaN, which does
-// not count for e.  Held as e + 127, a float's exponent field.  Every value that a block stands for is an FP16 value: a code has seven
+// not count for e.  Held as e + 127, a float's exponent field, plus kKeepNan in a block with a NaN: a reader of the scale knows whether to look
+// for its code.  Every value that a block stands for is an FP16 value: a code has seven
 // bits and 2^-24 is FP16's smallest step (FP16 values below it do not exist, so the lower limit rounds none of them).
 constexpr int kKeepBlock = 32;
-constexpr int kKeepLeast = 127 - 24, kKeepMost = 127 + 9;
+constexpr int kKeepLeast = 127 - 24, kKeepMost = 127 + 9, kKeepNan = 64;
 constexpr float kKeepClip = 127.5f * 512.0f;
 
 // the step's exponent field for the block's largest magnitude (no NaN): 255/128 and more of a power of two take the next step
@@ -81,16 +83,23 @@ __device__ __forceinline__ int keep_codes_any(float a, float b, float c, float d
   return keep_code_any(a, inverse) | (keep_code_any(b, inverse) << 8) | (keep_code_any(c, inverse) << 16) | (keep_code_any(d, inverse) << 24);
 }
 
-// what code number I of a word stands for
-template <int I>
-__device__ __forceinline__ float keep_value(int word, float step) {
-  const int c = (int)((uint32_t)word << (24 - 8 * I)) >> 24;
-  return (float)c * step;
+// The values of eight codes, times `factor`: as unsigned bytes 128 higher, for which there is a conversion per byte.  One fused multiply-add
+// takes the 128 off again (exact for a factor of one).
+__device__ __forceinline__ void keep_values(v2i codes, float step, float (&v)[8]) {
+  const float off = -128.0f * step;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t w = (uint32_t)codes[h] ^ 0x80808080u;
+    v[4 * h] = __builtin_fmaf((float)(w & 0xffu), step, off);
+    v[4 * h + 1] = __builtin_fmaf((float)(w >> 8 & 0xffu), step, off);
+    v[4 * h + 2] = __builtin_fmaf((float)(w >> 16 & 0xffu), step, off);
+    v[4 * h + 3] = __builtin_fmaf((float)(w >> 24), step, off);
+  }
 }
-// whether a word holds the code of a NaN
-__device__ __forceinline__ bool keep_has_nan(int word) {
-  const uint32_t x = (uint32_t)word ^ 0x80808080u;           // a zero byte
-  return ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
+__device__ __forceinline__ void keep_put_nan(v2i codes, float (&v)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (((uint32_t)codes[k / 4] >> (k % 4 * 8) & 0xffu) == 0x80u) v[k] = __builtin_nanf("");
 }
 
 }  // namespace us

@@ -47,6 +47,20 @@ __device__ __forceinline__ void store_section(const uint8_t* strip, void* to, ui
   }
 }
 
+// FP8 codes of four values that are known to be numbers within the type's range.
+template <int FMT>
+__device__ __forceinline__ int codes_in_range(const float* v) {
+  if constexpr (FMT == US_E4M3) return __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), true);
+  else return __builtin_amdgcn_cvt_pk_bf8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_bf8_f32(v[0], v[1], 0, false), true);
+}
+// The larger of m and the magnitudes of N values, NaN if one is (one instruction per two values).
+template <int N>
+__device__ __forceinline__ float most(float m, const float* v) {
+#pragma unroll
+  for (int k = 0; k < N; k += 2) m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, __builtin_fabsf(v[k])), __builtin_fabsf(v[k + 1]));
+  return m;
+}
+
 // Largest magnitude of a row's 32 values: a lane has `own`, the others are in the lanes 16 and 32 (16 x 16 results) or 32 (32 x 32) apart.
 template <bool M16>
 __device__ __forceinline__ float row_max_across(float own, bool ignore_nan) {
@@ -80,9 +94,14 @@ __device__ __forceinline__ uint32_t keep_quads(const v4f (&z)[NQ], int (&code)[N
       for (int e = 0; e < 4; ++e) m = __builtin_fmaxf(m, __builtin_fabsf(z[q][e]));
     m = row_max_across<M16>(m, true);
     const uint32_t s = keep_scale(m);
+    bool nan = false;
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) code[q] = keep_codes_any(z[q][0], z[q][1], z[q][2], z[q][3], keep_inverse(s));
-    return s;
+    for (int q = 0; q < NQ; ++q) {
+      code[q] = keep_codes_any(z[q][0], z[q][1], z[q][2], z[q][3], keep_inverse(s));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) nan |= z[q][e] != z[q][e];
+    }
+    return s + (row_max_across<M16>(nan ? 1.0f : 0.0f, true) != 0.0f ? kKeepNan : 0);
   }
   const uint32_t s = keep_scale(m);
   const float inv = keep_inverse(s);
@@ -117,20 +136,34 @@ __device__ __forceinline__ void gate_epilogue(const GemmArgs& g, const Acc& acc,
 #pragma unroll
         for (int h = 0; h < 4 / NQ; ++h) {                                      // groups of quads of one row
           v4f zg[NQ], zu[NQ];
+          float y[NQ][4];
           const int row = Acc::row(h * NQ, lane);
           uint8_t* const p = strip + row * EP;
 #pragma unroll
           for (int q = 0; q < NQ; ++q) {
             zg[q] = acc.quad(I0 + i, j, h * NQ + q) * g.scale;
             zu[q] = acc.quad(I0 + i, HJ + j, h * NQ + q) * g.scale;
-            const int col = j * 32 + Acc::col(h * NQ + q, lane);
-            float y[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = g.epi_scale * gate_terms<GATE>(zg[q][e]).f * zu[q][e];
-            if constexpr (FP8) {
-              *US_LDS_PTR(uint32_t, p + 2 * S::ZB + col) = cvt4_fp8<US_E4M3>(y[0], y[1], y[2], y[3]);
+            for (int e = 0; e < 4; ++e) y[q][e] = gate_terms<GATE>(zg[q][e]).f * (zu[q][e] * g.epi_scale);
+          }
+          if constexpr (FP8) {
+            // a NaN or a value to clip is rare, so the wave looks for one first
+            int c[NQ];
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(most<NQ * 4>(0.0f, &y[0][0]) <= 448.0f)) != 0, 0)) {
+#pragma unroll
+              for (int q = 0; q < NQ; ++q) c[q] = (int)cvt4_fp8<US_E4M3>(y[q][0], y[q][1], y[q][2], y[q][3]);
             } else {
-              const v4h o = {to_half(y[0]), to_half(y[1]), to_half(y[2]), to_half(y[3])};
+#pragma unroll
+              for (int q = 0; q < NQ; ++q) c[q] = codes_in_range<US_E4M3>(y[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) *US_LDS_PTR(int, p + 2 * S::ZB + j * 32 + Acc::col(h * NQ + q, lane)) = c[q];
+          }
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+            const int col = j * 32 + Acc::col(h * NQ + q, lane);
+            if constexpr (!FP8) {
+              const v4h o = {to_half(y[q][0]), to_half(y[q][1]), to_half(y[q][2]), to_half(y[q][3])};
               *US_LDS_PTR(v4h, p + 2 * S::ZB + col * 2) = o;
             }
             if constexpr (!KEEP8) {
@@ -174,40 +207,17 @@ __device__ __forceinline__ void gate_epilogue(const GemmArgs& g, const Acc& acc,
   });
 }
 
-// dZ (and H) of eight consecutive columns.
-template <int GATE, bool FP8, bool WITH_H>
-__device__ __forceinline__ void gate_gradients(const GemmArgs& g, const float (&dh)[8], const float (&zg)[8], const float (&zu)[8], v8h (&half)[3], v2i (&code)[3]) {
-  float r[3][8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const GateTerms t = gate_terms<GATE>(zg[k]);
-    r[0][k] = g.epi_scale * t.slope * zu[k] * dh[k];
-    r[1][k] = g.skip_scale * t.f * dh[k];
-    r[2][k] = g.gate_alpha * t.f * zu[k];
-  }
-#pragma unroll
-  for (int w = 0; w < (WITH_H ? 3 : 2); ++w) {
-    if constexpr (FP8) {
-      if (w < 2) code[w] = v2i{(int)cvt4_fp8<US_E5M2>(r[w][0], r[w][1], r[w][2], r[w][3]), (int)cvt4_fp8<US_E5M2>(r[w][4], r[w][5], r[w][6], r[w][7])};
-      else code[w] = v2i{(int)cvt4_fp8<US_E4M3>(r[w][0], r[w][1], r[w][2], r[w][3]), (int)cvt4_fp8<US_E4M3>(r[w][4], r[w][5], r[w][6], r[w][7])};
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) half[w][k] = to_half(r[w][k]);
-    }
-  }
-}
-
-// Zg and Zu of eight consecutive columns as they were kept.
+// Zg and Zu (times `factor`) of eight consecutive columns as they were kept.
 template <bool KEEP8>
 struct KeptPair;
 template <>
 struct KeptPair<false> {
   v8h zg, zu;
-  __device__ __forceinline__ void get(float (&a)[8], float (&b)[8]) const {
+  __device__ __forceinline__ void get(float factor, float (&a)[8], float (&b)[8]) const {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       a[k] = (float)zg[k];
-      b[k] = (float)zu[k];
+      b[k] = __builtin_fmaf((float)zu[k], factor, -0.0f);       // one mixed instruction
     }
   }
 };
@@ -215,21 +225,57 @@ template <>
 struct KeptPair<true> {
   v2i zg, zu;
   uint32_t sg, su;
-  __device__ __forceinline__ static void values(v2i c, uint32_t s, float (&v)[8]) {
-    const float step = keep_step(s);
-    v[0] = keep_value<0>(c.x, step); v[1] = keep_value<1>(c.x, step); v[2] = keep_value<2>(c.x, step); v[3] = keep_value<3>(c.x, step);
-    v[4] = keep_value<0>(c.y, step); v[5] = keep_value<1>(c.y, step); v[6] = keep_value<2>(c.y, step); v[7] = keep_value<3>(c.y, step);
-    if (__builtin_amdgcn_ballot_w64(keep_has_nan(c.x) || keep_has_nan(c.y)) != 0) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (((k < 4 ? c.x : c.y) >> (k % 4 * 8) & 0xff) == 0x80) v[k] = __builtin_nanf("");
+  __device__ __forceinline__ void get(float factor, float (&a)[8], float (&b)[8]) const {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(sg > kKeepMost || su > kKeepMost) != 0, 0)) {      // a block with a NaN
+      keep_values(zg, keep_step(sg > kKeepMost ? sg - kKeepNan : sg), a);
+      keep_values(zu, keep_step(su > kKeepMost ? su - kKeepNan : su) * factor, b);
+      if (sg > kKeepMost) keep_put_nan(zg, a);
+      if (su > kKeepMost) keep_put_nan(zu, b);
+      return;
     }
-  }
-  __device__ __forceinline__ void get(float (&a)[8], float (&b)[8]) const {
-    values(zg, sg, a);
-    values(zu, su, b);
+    keep_values(zg, keep_step(sg), a);
+    keep_values(zu, keep_step(su) * factor, b);
   }
 };
+
+// dZ (and H) of eight consecutive columns.  dh comes with dZ's second factor (beta_up) in it, and the first one's ratio to it goes into Zu, so that the
+// three results take five products: [f' (k Zu) dh | f dh] and H = f (k Zu) (alpha / k), k = beta_gate / beta_up.
+struct GateFactors {
+  float up, k, h;      // beta_up, beta_gate / beta_up, alpha / k
+  __device__ __forceinline__ explicit GateFactors(const GemmArgs& g) : up(g.skip_scale), k(g.epi_scale / g.skip_scale), h(g.gate_alpha * g.skip_scale / g.epi_scale) {}
+};
+template <int GATE, bool FP8, bool KEEP8>
+__device__ __forceinline__ void gate_gradients(const GateFactors& c, const float (&dh)[8], const KeptPair<KEEP8>& z, v8h (&half)[3], v2i (&code)[3]) {
+  constexpr int N = KEEP8 ? 3 : 2;
+  float zg[8], zu[8], r[3][8];
+  z.get(c.k, zg, zu);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const GateTerms t = gate_terms<GATE>(zg[k]);
+    r[0][k] = t.slope * (zu[k] * dh[k]);
+    r[1][k] = t.f * dh[k];
+    r[2][k] = t.f * zu[k] * c.h;
+  }
+  if constexpr (FP8) {
+    // a NaN or a value to clip is rare, so the wave looks for one first
+    const float m = most<8>(most<8>(0.0f, r[0]), r[1]), mh = KEEP8 ? most<8>(0.0f, r[2]) : 0.0f;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(m <= 57344.0f && mh <= 448.0f)) != 0, 0)) {
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+        code[w] = v2i{(int)cvt4_fp8<US_E5M2>(r[w][0], r[w][1], r[w][2], r[w][3]), (int)cvt4_fp8<US_E5M2>(r[w][4], r[w][5], r[w][6], r[w][7])};
+      if constexpr (KEEP8) code[2] = v2i{(int)cvt4_fp8<US_E4M3>(r[2][0], r[2][1], r[2][2], r[2][3]), (int)cvt4_fp8<US_E4M3>(r[2][4], r[2][5], r[2][6], r[2][7])};
+    } else {
+#pragma unroll
+      for (int w = 0; w < 2; ++w) code[w] = v2i{codes_in_range<US_E5M2>(r[w]), codes_in_range<US_E5M2>(r[w] + 4)};
+      if constexpr (KEEP8) code[2] = v2i{codes_in_range<US_E4M3>(r[2]), codes_in_range<US_E4M3>(r[2] + 4)};
+    }
+  } else {
+#pragma unroll
+    for (int w = 0; w < N; ++w)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) half[w][k] = to_half(r[w][k]);
+  }
+}
 
 // Backward.  g.ldc: row pitch of Z and dZ (2f).
 template <class Cfg, bool FP8, int EPI, int I0, int I1, class Acc>
@@ -294,6 +340,8 @@ __device__ __forceinline__ void gate_grad_epilogue(const GemmArgs& g, const Acc&
     }
   };
   fetch_group(0);
+  const GateFactors factors(g);
+  const float scale = g.scale * factors.up;
   with_gate(g.act, [&](auto gate) {
     constexpr int GATE = decltype(gate)::value;
 #pragma unroll
@@ -301,7 +349,7 @@ __device__ __forceinline__ void gate_grad_epilogue(const GemmArgs& g, const Acc&
 #pragma unroll
       for (int j = 0; j < Cfg::FN; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) *US_LDS_PTR(v4f, strip + Acc::row(q, lane) * EP + (j * 32 + Acc::col(q, lane)) * 4) = acc.quad(I0 + i, j, q) * g.scale;
+        for (int q = 0; q < 4; ++q) *US_LDS_PTR(v4f, strip + Acc::row(q, lane) * EP + (j * 32 + Acc::col(q, lane)) * 4) = acc.quad(I0 + i, j, q) * scale;
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       if (i % ZGROUP == 0) {
@@ -318,11 +366,9 @@ __device__ __forceinline__ void gate_grad_epilogue(const GemmArgs& g, const Acc&
         const uint8_t* p = strip + (u * RPP + lrow) * EP + lcol * 4;
         const v4f lo = *US_LDS_PTR(const v4f, p), hi = *US_LDS_PTR(const v4f, p + 16);
         const float dh[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        float zg[8], zu[8];
-        kept[i % ZGROUP][u].get(zg, zu);
         v8h half[3];
         v2i code[3];
-        gate_gradients<GATE, FP8, KEEP8>(g, dh, zg, zu, half, code);
+        gate_gradients<GATE, FP8, KEEP8>(factors, dh, kept[i % ZGROUP][u], half, code);
         const int dbelow = (int)((uint32_t)(u * RPP) * pitch * OES);
         [[maybe_unused]] const int hbelow = (int)((uint32_t)(u * RPP) * (uint32_t)f * OES);
         if constexpr (FP8) {
@@ -358,8 +404,9 @@ __device__ __forceinline__ void gate_point(const GemmArgs& g, long m, long n, bo
       }
       big = __builtin_fmaxf(big, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, big), 0xB1, 0xf, 0xf, true)));
       big = __builtin_fmaxf(big, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, big), 0x4E, 0xf, 0xf, true)));
-      const uint32_t s = keep_scale(big);
+      uint32_t s = keep_scale(big);
       const float inv = keep_inverse(s);
+      if (__builtin_amdgcn_ballot_w64(rare) >> (threadIdx.x & 60) & 15) s += kKeepNan;      // in any of the block's four lanes
       v2i c;
       if (rare || big >= kKeepClip) c = v2i{keep_codes_any(z[0], z[1], z[2], z[3], inv), keep_codes_any(z[4], z[5], z[6], z[7], inv)};
       else c = v2i{keep_codes(z[0], z[1], z[2], z[3], inv), keep_codes(z[4], z[5], z[6], z[7], inv)};
@@ -381,7 +428,7 @@ __device__ __forceinline__ void gate_point(const GemmArgs& g, long m, long n, bo
   if (!in) return;
   float y[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) y[k] = g.epi_scale * gate_terms<GATE>(zg[k]).f * zu[k];
+  for (int k = 0; k < 8; ++k) y[k] = gate_terms<GATE>(zg[k]).f * (zu[k] * g.epi_scale);
   if constexpr (FP8) {
     const v2i c = {(int)cvt4_fp8<US_E4M3>(y[0], y[1], y[2], y[3]), (int)cvt4_fp8<US_E4M3>(y[4], y[5], y[6], y[7])};
     wt_store(reinterpret_cast<v2i*>((uint8_t*)g.gate_h + m * f + n), c);
@@ -408,11 +455,13 @@ __device__ __forceinline__ void gate_grad_point(const GemmArgs& g, long m, long 
     z.zg = *reinterpret_cast<const v8h*>(g.Zpre + m * g.ldc + n);
     z.zu = *reinterpret_cast<const v8h*>(g.Zpre + m * g.ldc + f + n);
   }
-  float zg[8], zu[8];
-  z.get(zg, zu);
+  const GateFactors factors(g);
+  float up[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) up[k] = dh[k] * factors.up;
   v8h half[3];
   v2i code[3];
-  gate_gradients<GATE, FP8, KEEP8>(g, dh, zg, zu, half, code);
+  gate_gradients<GATE, FP8, KEEP8>(factors, up, z, half, code);
   if constexpr (FP8) {
     wt_store(reinterpret_cast<v2i*>(g.aux8 + m * g.ldc + n), code[0]);
     wt_store(reinterpret_cast<v2i*>(g.aux8 + m * g.ldc + f + n), code[1]);

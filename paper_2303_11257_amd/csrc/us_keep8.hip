@@ -34,8 +34,11 @@ __global__ void __launch_bounds__(kThreads) keep8_store_kernel(const _Float16* _
       rare |= x[k] != x[k];
     }
     m = quad_max(m);
-    const uint32_t s = keep_scale(m);
+    uint32_t s = keep_scale(m);
     const float inv = keep_inverse(s);
+    // a NaN in any of the block's four lanes
+    const uint64_t nans = __builtin_amdgcn_ballot_w64(rare) >> (threadIdx.x & 60) & 15;
+    if (nans) s += kKeepNan;
     v2i c;
     if (rare || m >= kKeepClip) {
       c.x = keep_codes_any((float)x[0], (float)x[1], (float)x[2], (float)x[3], inv);
@@ -57,14 +60,13 @@ __global__ void __launch_bounds__(kThreads) keep8_load_kernel(const int8_t* __re
   if (col >= n) return;
   for (long r = blockIdx.y; r < rows; r += gridDim.y) {
     const v2i c = *reinterpret_cast<const v2i*>(codes + r * n + col);
-    const float step = keep_step(scales[r * blocks + (chunk >> 2)]);
-    v8h x = {(_Float16)keep_value<0>(c.x, step), (_Float16)keep_value<1>(c.x, step), (_Float16)keep_value<2>(c.x, step), (_Float16)keep_value<3>(c.x, step),
-             (_Float16)keep_value<0>(c.y, step), (_Float16)keep_value<1>(c.y, step), (_Float16)keep_value<2>(c.y, step), (_Float16)keep_value<3>(c.y, step)};
-    if (keep_has_nan(c.x) || keep_has_nan(c.y)) {
+    const uint32_t s = scales[r * blocks + (chunk >> 2)];
+    float v[8];
+    keep_values(c, keep_step(s > kKeepMost ? s - kKeepNan : s), v);
+    if (s > kKeepMost) keep_put_nan(c, v);
+    v8h x;
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (((k < 4 ? c.x : c.y) >> (k % 4 * 8) & 0xff) == 0x80) x[k] = half_from_bits(0x7e00);
-    }
+    for (int k = 0; k < 8; ++k) x[k] = (_Float16)v[k];
     *reinterpret_cast<v8h*>(X + r * ld + col) = x;
   }
 }

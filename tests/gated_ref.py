@@ -25,7 +25,8 @@ def gate_slope(gate, z):
 
 
 def keep8(x):
-    """[rows, n] float64 -> (codes int8, scales uint8): blocks of 32 of a row, step 2^e, e the smallest of -24 .. 9 with max|x| < 127.5 2^e."""
+    """[rows, n] float64 -> (codes int8, scales uint8): blocks of 32 of a row, step 2^e, e the smallest of -24 .. 9 with max|x| < 127.5 2^e; the scale is
+    e + 127, with 64 more for a block that holds a NaN."""
     x = np.asarray(x, dtype=np.float64)
     rows, n = x.shape
     nb = -(-n // 32)
@@ -39,12 +40,12 @@ def keep8(x):
     with np.errstate(invalid="ignore"):
         q = np.clip(np.rint(b / 2.0 ** e[..., None]), -127, 127)
     q = np.where(np.isnan(b), -128, q).astype(np.int8)
-    return q.reshape(rows, nb * 32)[:, :n].copy(), (e + 127).astype(np.uint8)
+    return q.reshape(rows, nb * 32)[:, :n].copy(), (e + 127 + 64 * np.isnan(b).any(2)).astype(np.uint8)
 
 
 def keep8_values(codes, scales):
     n = codes.shape[1]
-    step = np.repeat(2.0 ** (scales.astype(np.float64) - 127), 32, axis=1)[:, :n]
+    step = np.repeat(2.0 ** (scales.astype(np.float64) - 127 - 64 * (scales > 136)), 32, axis=1)[:, :n]
     return np.where(codes == -128, np.nan, codes.astype(np.float64) * step)
 
 

