@@ -20,7 +20,12 @@ hipError_t launch_gate(const GemmProblem& p, hipStream_t st) {
   if (c == SmallTileChoice::T32x32 || c == SmallTileChoice::T32x64 || (c == SmallTileChoice::None && p.M <= 32)) return launch_small<CfgT32x64, FP8, FA, 0, true, NT, EPI, false>(p, st);
   if (c == SmallTileChoice::T64x64) return launch_small<CfgT64x64, FP8, FA, 0, true, NT, EPI, false>(p, st);
   using Big = typename std::conditional<!NT && (FP8 || EPI == EPI_GATE8), CfgG256, CfgD256>::type;
-  if (use_big_tile(p.M, p.N, 1)) return launch_one<true, Big, FP8, FA, 0, true, NT, EPI, false>(p, 1, p.K, st);
+  // dH with Z in FP16 and a short reduction: two workgroups per CU, one of which reads its Z and stores its dZ under the other's products, where large
+  // tiles all read at once.  us, dZ alone, D256 -> D128: FP8 8192 x K x 4096, K = 512 72.1 -> 52.8, 1024 82.1 -> 64.8, 2048 100 -> 89, 2560 115 -> 108,
+  // 4096 x 4096 x 4096 71.5 -> 74.4; FP16 K = 512 96 -> 75, 1024 111 -> 109, 2048 161 -> 162; with 8-bit blocks, half of the bytes, FP8 K = 512 54.5 -> 56.1,
+  // 1024 64.6 -> 68.9, FP16 1024 98 -> 108: not taken
+  const bool two_per_cu = EPI == EPI_GATE_GRAD && p.K * (FP8 ? 1 : 2) <= 2560;
+  if (use_big_tile(p.M, p.N, 1) && !two_per_cu) return launch_one<true, Big, FP8, FA, 0, true, NT, EPI, false>(p, 1, p.K, st);
   return launch_one<true, CfgD128, FP8, FA, 0, true, NT, EPI, false>(p, 1, p.K, st);
 }
 
