@@ -798,6 +798,22 @@ us_status us_ffn_gated_bwd(const void* X, const void* Wgu, const void* Wd, const
     const bool go = pass == 1;
     if (go && T > 0) {
       if (us_status s = from_hip(gemm_gate_grad(p, keep8, as_stream(stream))); s != US_OK) return s;
+      // all three products behind dZ together
+      if (dX && dWgu && dWd) {
+        auto product = [](const void* A, const void* B, void* C, long M, long N, long K, long lda, long ldb, bool kc, us_dtype a, us_dtype b, long fan) {
+          GemmProblem q{};
+          q.A = A; q.B = B; q.C = C;
+          q.M = M; q.N = N; q.K = K;
+          q.lda = lda; q.ldb = ldb; q.ldc = N;
+          q.a_kc = q.b_kc = kc;
+          q.a_dt = a; q.b_dt = b; q.c_dt = US_F16;
+          q.scale = (float)(1.0 / sqrt((double)fan));
+          return q;
+        };
+        const GemmProblem dx = product(dZ, Wgu, dX, T, d, 2 * f, 2 * f, 2 * f, true, gr, op, 2 * f);
+        const GemmProblem dwgu = product(X, dZ, dWgu, d, 2 * f, T, d, 2 * f, false, op, gr, T), dwd = product(H, G, dWd, f, d, T, f, d, false, op, gr, T);
+        if (gemm_gate_three_ok(dx, dwgu, dwd)) return from_hip(gemm_gate_three(dx, dwgu, dwd, as_stream(stream)));
+      }
     }
     // dWd = T^-1/2 H^T G; dX = (2f)^-1/2 dZ Wgu^T and dWgu = T^-1/2 X^T dZ (no tokens: gradients of zero)
     us_status s = linear_bwd_impl(H, Wd, G, nullptr, dWd, T, f, d, op, op, gr, US_F16, 0.0f, 0.0f, US_EPI_NONE, 0.0f, nullptr, nullptr, workspace,

@@ -9,5 +9,8 @@ hipError_t gemm_gate_fwd_f16(const GemmProblem& p, bool keep8, hipStream_t st) {
 hipError_t gemm_gate_grad_f16(const GemmProblem& p, bool keep8, hipStream_t st) {
   return keep8 ? launch_gate<false, true, EPI_GATE8_GRAD>(p, st) : launch_gate<false, true, EPI_GATE_GRAD>(p, st);
 }
+hipError_t gemm_gate_three_f16(const GemmProblem& dx, const GemmProblem& dwgu, const GemmProblem& dwd, hipStream_t st) {
+  return launch_three_grads<false>(dx, dwgu, dwd, st);
+}
 
 }  // namespace us

@@ -9,5 +9,8 @@ hipError_t gemm_gate_fwd_fp8(const GemmProblem& p, bool keep8, hipStream_t st) {
 hipError_t gemm_gate_grad_fp8(const GemmProblem& p, bool keep8, hipStream_t st) {
   return keep8 ? launch_gate<true, true, EPI_GATE8_GRAD>(p, st) : launch_gate<true, true, EPI_GATE_GRAD>(p, st);
 }
+hipError_t gemm_gate_three_fp8(const GemmProblem& dx, const GemmProblem& dwgu, const GemmProblem& dwd, hipStream_t st) {
+  return launch_three_grads<true>(dx, dwgu, dwd, st);
+}
 
 }  // namespace us

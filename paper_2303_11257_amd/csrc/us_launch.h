@@ -169,6 +169,9 @@ hipError_t launch_gemm(const GemmProblem& p, hipStream_t stream);
 bool gemm_gate_offsets_fit(const GemmProblem& p);
 hipError_t gemm_gate_fwd(const GemmProblem& p, bool keep8, hipStream_t stream);
 hipError_t gemm_gate_grad(const GemmProblem& p, bool keep8, hipStream_t stream);
+// The gated block's gradients behind dZ in one launch, where gemm_gate_three_ok.
+bool gemm_gate_three_ok(const GemmProblem& dx, const GemmProblem& dwgu, const GemmProblem& dwd);
+hipError_t gemm_gate_three(const GemmProblem& dx, const GemmProblem& dwgu, const GemmProblem& dwd, hipStream_t stream);
 // The gated block's projections for a few rows (us_gemm_rows.hip), where gemm_rows_take: `up` as gemm_gate_fwd takes it, `down` the second projection of
 // its H, FP16 result [M,N] in C.  partial: gemm_rows_workspace_bytes, 0 where the block does not take them.
 constexpr long kRowsMost = 8, kMostSteps = 16;      // kMostSteps: steps of 64 rows in a slice, whose part of X lies in LDS

@@ -321,3 +321,40 @@ def test_unit_variance():
     for n in ("Z", "H", "Y", "dX", "dWgu", "dWd"):
         assert abs(float(out[n][:-1].double().square().mean()) - 1) < 0.05, n
     assert abs(float(out["dZ"][:-1].double().square().mean()) - 1) < 0.05
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,d,f,forward,dz,grads", [
+    (100, 256, 688, "32x64", "32x64", "three:32x64"),            # few tiles everywhere
+    (700, 1040, 1552, "128x128:wk2", "128x128", None),           # two wave groups where the reduction has 2048 bytes (FP16)
+    (1900, 256, 2064, "128x128", "128x128", None),
+    (2064, 784, 2080, "256x256", "128x128", None),               # one round of large tiles instead of two of small ones
+    (1333, 1248, 2496, None, None, "three:128x128"),
+    (11000, 272, 2064, "256x256", "128x128", None),               # dZ with a short reduction: two workgroups per CU
+])
+def test_tiles_by_rule(T, d, f, forward, dz, grads, fp8):
+    """One block inside every window of the choice of tiles; the results go by the definition whichever is taken."""
+    for keep8 in (False, True):
+        b = Block(T, d, f, fp8, keep8, us.GATE_SILU, seed=5)
+        first = b.forward().outputs()
+        taken = us.last_launch().split(" + ")[0]
+        if forward and not (fp8 and ":wk2" in forward):
+            assert forward in taken, taken
+        check_forward(b, first)
+        out = b.backward().outputs()
+        launches = us.last_launch().split(" + ")
+        if dz and not keep8:
+            assert dz in launches[0], launches
+        if grads:
+            assert len(launches) == 4 and all(n.startswith(grads) for n in launches[1:]), launches
+        check_backward(b, out)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_wide_gradients_on_large_tiles(fp8):
+    """dZ on large tiles (a long reduction in FP8 bytes, or 8-bit blocks), rows and columns that end inside a tile."""
+    for T, d, f, keep8 in ((3000, 2576, 4112, False), (3000, 144, 4112, True)):
+        b = Block(T, d, f, fp8, keep8, us.GATE_GELU, seed=6)
+        b.forward().backward()
+        assert us.last_launch().startswith("direct:256x256"), us.last_launch()
+        check_backward(b, b.outputs())
