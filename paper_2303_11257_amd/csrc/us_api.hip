@@ -761,9 +761,11 @@ us_status us_ffn_gated_fwd(const void* X, const void* Wgu, const void* Wd, void*
   q.a_kc = true; q.b_kc = false;
   q.a_dt = op; q.b_dt = op; q.c_dt = US_F16;
   q.scale = (float)(1.0 / sqrt((double)f));
-  if (workspace && gemm_rows_take(T, d, f, fp8) && workspace_bytes >= gemm_rows_workspace_bytes(T, d, f, fp8))
-    return from_hip(gemm_rows_ffn(p, q, keep8, workspace, as_stream(stream)));
-  if (us_status s = from_hip(gemm_gate_fwd(p, keep8, as_stream(stream))); s != US_OK) return s;
+  const bool room = workspace && workspace_bytes >= gemm_rows_workspace_bytes(T, d, f, fp8);
+  if (room && gemm_rows_take(T, d, f, fp8)) return from_hip(gemm_rows_ffn(p, q, keep8, workspace, as_stream(stream)));
+  const int up = room ? gemm_up_slices(T, d, f, fp8) : 1, down = room ? gemm_down_slices(T, d, f, fp8) : 1;
+  if (us_status s = from_hip(up > 1 ? gemm_small_gate(p, up, keep8, workspace, as_stream(stream)) : gemm_gate_fwd(p, keep8, as_stream(stream))); s != US_OK) return s;
+  if (down > 1) return from_hip(gemm_small_store(q, down, workspace, as_stream(stream)));
   return linear_fwd_impl(H, Wd, nullptr, Y, T, f, d, op, op, US_F16, 0.0f, US_EPI_NONE, 0.0f, nullptr, nullptr, nullptr, 0, stream, true, true);
 }
 

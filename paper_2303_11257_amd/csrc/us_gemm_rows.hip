@@ -1,6 +1,7 @@
-// Products of at most eight rows (the tokens of one generation step) with a weight matrix, for the gated block's two projections.
+// Products of a few rows (the tokens of one generation step) with a weight matrix, for the gated block's two projections: as streams of the
+// weights (one to eight rows), and on the few-tiles kernel with the reduction in slices (up to 64).
 //
-// Y = X W with X [T,K], T <= 8 (FP8: 4), W [K,N] row-major.  What bounds it: every weight is read once from HBM and used T times, so nothing but the rate of
+// Streams.  Y = X W with X [T,K], T <= 8 (FP8: 4), W [K,N] row-major.  What bounds it: every weight is read once from HBM and used T times, so nothing but the rate of
 // that stream counts.  Weights go from memory to registers in 16-byte loads and into FP32 multiply-adds there: no LDS, no matrix
 // instructions, whose operands would have to be transposed on the way.  (FP16: v_fma_mix takes the halves as they are; FP8: two values per
 // conversion.  Per 16 bytes of weights of a lane 8 T, FP8 8 + 16 T instructions.)
@@ -224,8 +225,35 @@ bool gemm_rows_take(long T, long d, long f, bool fp8) {
   // (a slice's rows are addressed with 32-bit offsets)
   return T >= 1 && T <= most && 2 * f * es < (1l << 31) / (kMostSteps * kBatch) && d * es < (1l << 31) / (kMostSteps * kBatch);
 }
+// Slices of a product of at most kSliceRows rows on the few-tiles kernel: the number that leaves the least of the last round empty (`tile`: columns of a
+// tile, of which `per_cu` fit on a CU), each with at least 1024 bytes of the reduction; 1 where they would not save a quarter, where the weights are
+// below 4 MB (the second kernel costs what they save), and for more than 32 rows unless there are four (unsliced, such a product
+// takes a taller tile and reads its weights once).  us, forward call without Z, unsliced -> this rule (slices of up, down):
+//   FP16 2048 x 5632 T = 9 38.5 -> 28.7 (1, 8), 32 44.9 -> 32.6, 64 44.5 -> 38.9 (1, 4); 4096 x 11008 T = 13 102 -> 80 (5, 4), 32 116 -> 90; 1536 x 4096 T = 13 22.5 -> 20.2;
+//   FP8 4096 x 11008 T = 9 77 -> 66 (1, 4), 2048 x 5632 T = 13 22.5 -> 20.1 (1, 5); not taken: FP16 512 x 1376 11.0 -> 11.9 (1, 2), FP8 4096 x 11008 T = 64 76 -> 81 (1, 2)
+long slice_length(long K, int slices) { return ceil_div(ceil_div(K, slices), 64) * 64; }
+int gemm_small_slices(long T, long K, long N, bool fp8, int tile, int per_cu) {
+  if (T < 1 || T > kSliceRows || K * N * (fp8 ? 1 : 2) < (4l << 20)) return 1;
+  const long tiles = ceil_div(T, 32) * ceil_div(N, tile), slots = per_cu * cu_count(), most = K * (fp8 ? 1 : 2) / 1024;
+  int best = 1;
+  double least = (double)ceil_div(tiles, slots) * 0.75;
+  for (int s = 2; s <= 16 && s <= most; ++s) {
+    const double t = (double)ceil_div(tiles * s, slots) / s;
+    if (t < least * 0.97) {
+      best = s;
+      least = t;
+    }
+  }
+  return best == 1 || (T > 32 && best < 4) ? 1 : (int)ceil_div(K, slice_length(K, best));
+}
+int gemm_up_slices(long T, long d, long f, bool fp8) { return gemm_small_slices(T, d, 2 * f, fp8, 64, 1); }
+int gemm_down_slices(long T, long d, long f, bool fp8) { return gemm_small_slices(T, f, d, fp8, 32, 2); }
+
 size_t gemm_rows_workspace_bytes(long T, long d, long f, bool fp8) {
-  if (!gemm_rows_take(T, d, f, fp8)) return 0;
+  if (!gemm_rows_take(T, d, f, fp8)) {
+    const long u = gemm_up_slices(T, d, f, fp8), v = gemm_down_slices(T, d, f, fp8), a = u > 1 ? u * 2 * f : 0, b = v > 1 ? v * d : 0;
+    return T < 1 ? 0 : (size_t)T * (size_t)(a > b ? a : b) * sizeof(float);
+  }
   const long up = ceil_div(d, slice_rows(T, d, 2 * f, fp8)) * 2 * f, down = ceil_div(f, slice_rows(T, f, d, fp8)) * d;
   return (size_t)T * (size_t)(up > down ? up : down) * sizeof(float);
 }
@@ -258,18 +286,41 @@ hipError_t launch_rows(const GemmProblem& p, float* partial, hipStream_t st, int
   return hipErrorInvalidValue;
 }
 
-// Both projections.
+// The first projection's or the second one's sums in slices, and what makes Z and H or Y of them.
 template <bool FP8>
-hipError_t launch_rows_ffn(const GemmProblem& up, const GemmProblem& down, bool keep8, float* partial, hipStream_t st) {
-  int slices = 0;
-  if (hipError_t e = launch_rows<FP8>(up, partial, st, &slices); e != hipSuccess) return e;
+hipError_t launch_gate_of_sums(const GemmProblem& up, bool keep8, const float* partial, int slices, hipStream_t st) {
   const dim3 grid((unsigned)ceil_div(up.N / 2, 64), (unsigned)up.M);
   const GemmArgs g = make_args(up, up.K, 64, 64);
   if (keep8) rows_gate_kernel<EPI_GATE8, FP8><<<grid, 64, 0, st>>>(partial, g, slices);
   else rows_gate_kernel<EPI_GATE, FP8><<<grid, 64, 0, st>>>(partial, g, slices);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (hipError_t e = launch_rows<FP8>(down, partial, st, &slices); e != hipSuccess) return e;
+  return hipGetLastError();
+}
+hipError_t launch_store_of_sums(const GemmProblem& down, const float* partial, int slices, hipStream_t st) {
   rows_store_kernel<<<dim3((unsigned)ceil_div(down.N, 64), (unsigned)down.M), 64, 0, st>>>(partial, (_Float16*)down.C, (int)down.M, down.N, slices, down.scale);
+  return hipGetLastError();
+}
+
+// Both projections as streams.
+template <bool FP8>
+hipError_t launch_rows_ffn(const GemmProblem& up, const GemmProblem& down, bool keep8, float* partial, hipStream_t st) {
+  int slices = 0;
+  if (hipError_t e = launch_rows<FP8>(up, partial, st, &slices); e != hipSuccess) return e;
+  if (hipError_t e = launch_gate_of_sums<FP8>(up, keep8, partial, slices, st); e != hipSuccess) return e;
+  if (hipError_t e = launch_rows<FP8>(down, partial, st, &slices); e != hipSuccess) return e;
+  return launch_store_of_sums(down, partial, slices, st);
+}
+
+// A product on the few-tiles kernel with its reduction in slices, FP32 sums.
+template <class Cfg, bool FP8>
+hipError_t launch_small_slices(const GemmProblem& p, int slices, float* partial, hipStream_t st) {
+  constexpr int LDS = SmallTile<Cfg, FP8, true, false>::LDS_BYTES;
+  auto kern = gemm_small_kernel<Cfg, FP8, 0, 0, true, false, EPI_PARTIAL, true>;
+  note_gemm_launch("direct", Cfg::BM, Cfg::BN, Cfg::WAVES, Cfg::NST, FP8, true, false, EPI_PARTIAL, true, slices);
+  static FuncConfig cfg;
+  if (hipError_t e = cfg.ensure((const void*)kern, LDS); e != hipSuccess) return e;
+  GemmArgs g = make_args(p, slice_length(p.K, slices), Cfg::BM, Cfg::BN);
+  g.partial = partial;
+  kern<<<dim3((unsigned)(ceil_div(p.M, Cfg::BM) * ceil_div(p.N, Cfg::BN)), (unsigned)slices), Cfg::THREADS, LDS, st>>>(g);
   return hipGetLastError();
 }
 
@@ -277,6 +328,18 @@ hipError_t launch_rows_ffn(const GemmProblem& up, const GemmProblem& down, bool 
 
 hipError_t gemm_rows_ffn(const GemmProblem& up, const GemmProblem& down, bool keep8, void* partial, hipStream_t st) {
   return up.a_dt == US_F16 ? launch_rows_ffn<false>(up, down, keep8, (float*)partial, st) : launch_rows_ffn<true>(up, down, keep8, (float*)partial, st);
+}
+
+hipError_t gemm_small_gate(const GemmProblem& up, int slices, bool keep8, void* partial, hipStream_t st) {
+  const bool fp8 = up.a_dt != US_F16;
+  const hipError_t e = fp8 ? launch_small_slices<CfgT32x64, true>(up, slices, (float*)partial, st) : launch_small_slices<CfgT32x64, false>(up, slices, (float*)partial, st);
+  if (e != hipSuccess) return e;
+  return fp8 ? launch_gate_of_sums<true>(up, keep8, (const float*)partial, slices, st) : launch_gate_of_sums<false>(up, keep8, (const float*)partial, slices, st);
+}
+hipError_t gemm_small_store(const GemmProblem& down, int slices, void* partial, hipStream_t st) {
+  const hipError_t e = down.a_dt != US_F16 ? launch_small_slices<CfgT32x32, true>(down, slices, (float*)partial, st)
+                                           : launch_small_slices<CfgT32x32, false>(down, slices, (float*)partial, st);
+  return e != hipSuccess ? e : launch_store_of_sums(down, (const float*)partial, slices, st);
 }
 
 }  // namespace us

@@ -53,17 +53,20 @@ __device__ __forceinline__ void gemm_small_tile(const GemmArgs& g, int bid, uint
   const long m0 = (long)tm * BM, n0 = (long)tn * BN;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int nstages = (int)((g.K + T::BK - 1) / T::BK);
+  // EPI_PARTIAL: slice blockIdx.y of the reduction, FP32 sums
+  const long k0 = EPI == EPI_PARTIAL ? (long)blockIdx.y * g.k_per_split : 0;
+  const long klen = EPI == EPI_PARTIAL && g.K - k0 > g.k_per_split ? g.k_per_split : g.K - k0;
+  const int nstages = (int)((klen + T::BK - 1) / T::BK);
   uint8_t* ring = lds + wave * (NST * T::STAGE_BYTES);
 
   OperandLoads<64, BM, Cfg::BKB, A_KC, FP8, T::PA, T::A_LOADS, M16> la;
   OperandLoads<64, BN, Cfg::BKB, B_KC, FP8, T::PB, T::B_LOADS, M16> lb;
-  la.init(g.A, g.lda, m0, g.M, (long)wave * T::BK);
+  la.init(g.A, g.lda, m0, g.M, k0 + (long)wave * T::BK);
   if constexpr (is_gate(EPI)) lb.template init_gate<BN / 2>(g.B, g.ldb, n0 / 2, g.N / 2, (long)wave * T::BK);
-  else lb.init(g.B, g.ldb, n0, g.N, (long)wave * T::BK);
+  else lb.init(g.B, g.ldb, n0, g.N, k0 + (long)wave * T::BK);
   const long advA = W * (A_KC ? (long)Cfg::BKB : (long)T::BK * g.lda * T::ES);
   const long advB = W * (B_KC ? (long)Cfg::BKB : (long)T::BK * g.ldb * T::ES);
-  long kleft = g.K - (long)wave * T::BK;          // elements of the reduction from the next stage to request on
+  long kleft = klen - (long)wave * T::BK;         // elements of the reduction from the next stage to request on
   auto request = [&](int slot) {
     if (kleft < T::BK) {                          // the last stage, or none: the rest reads zeros from here on
       la.cut((int)kleft);
@@ -184,7 +187,11 @@ __device__ __forceinline__ void gemm_small_tile(const GemmArgs& g, int bid, uint
       lo += *US_LDS_PTR(const v4f, p);
       hi += *US_LDS_PTR(const v4f, p + 4);
     }
-    if constexpr (WIDE) {
+    if constexpr (EPI == EPI_PARTIAL) {
+      float* const to = g.partial + ((long)blockIdx.y * g.M + m) * g.N + n;
+      *reinterpret_cast<v4f*>(to) = lo;
+      *reinterpret_cast<v4f*>(to + 4) = hi;
+    } else if constexpr (WIDE) {
       lo *= g.scale;
       hi *= g.scale;
       wt_store(reinterpret_cast<v4f*>((float*)g.C + m * g.ldc + n), lo);

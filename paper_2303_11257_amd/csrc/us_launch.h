@@ -173,10 +173,16 @@ hipError_t gemm_gate_grad(const GemmProblem& p, bool keep8, hipStream_t stream);
 bool gemm_gate_three_ok(const GemmProblem& dx, const GemmProblem& dwgu, const GemmProblem& dwd);
 hipError_t gemm_gate_three(const GemmProblem& dx, const GemmProblem& dwgu, const GemmProblem& dwd, hipStream_t stream);
 // The gated block's projections for a few rows (us_gemm_rows.hip), where gemm_rows_take: `up` as gemm_gate_fwd takes it, `down` the second projection of
-// its H, FP16 result [M,N] in C.  partial: gemm_rows_workspace_bytes, 0 where the block does not take them.
+// its H, FP16 result [M,N] in C.  partial: gemm_rows_workspace_bytes, 0 where the block takes neither them nor slices.
 constexpr long kRowsMost = 8, kMostSteps = 16;      // kMostSteps: steps of 64 rows in a slice, whose part of X lies in LDS
 bool gemm_rows_take(long T, long d, long f, bool fp8);
 size_t gemm_rows_workspace_bytes(long T, long d, long f, bool fp8);
+// ... and for up to kSliceRows rows on the few-tiles kernel with its reduction in slices (1: not), sums in `partial` likewise.
+constexpr long kSliceRows = 64;
+int gemm_up_slices(long T, long d, long f, bool fp8);
+int gemm_down_slices(long T, long d, long f, bool fp8);
+hipError_t gemm_small_gate(const GemmProblem& up, int slices, bool keep8, void* partial, hipStream_t stream);
+hipError_t gemm_small_store(const GemmProblem& down, int slices, void* partial, hipStream_t stream);
 hipError_t gemm_rows_ffn(const GemmProblem& up, const GemmProblem& down, bool keep8, void* partial, hipStream_t stream);
 // Two batches of equally shaped FP16 products with both operands K-strided (attention's dV and dK) in one launch.
 hipError_t gemm_tn_f16_two_batches(const GemmProblem& p, const GemmProblem& q, hipStream_t stream);

@@ -226,6 +226,21 @@ def test_a_few_rows(T, fp8):
         assert "stream" not in us.last_launch()
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,d,f,up,down", [(9, 2064, 5648, False, True), (32, 4112, 5136, True, True), (33, 2048, 5632, False, True), (64, 1040, 4112, False, True),
+                                           (65, 1040, 4112, False, False), (17, 512, 1376, False, False)])
+def test_a_few_rows_in_slices(T, d, f, up, down, fp8):
+    """Up to 64 rows: reductions in slices on either side of the rule, the last slice shorter than the others."""
+    for keep8 in (False, True):
+        b = Block(T, d, f, fp8, keep8, us.GATE_SIGMOID, seed=T)
+        check_forward(b, b.forward().outputs())
+        launches = us.last_launch().split(" + ")
+        if not fp8:
+            assert ["partial" in n for n in launches] == [up, down], launches
+        check_forward(b, b.forward(ws=False).outputs())
+        assert "partial" not in us.last_launch()
+
+
 def test_single_gradients_and_none_of_no_tokens():
     b = Block(130, 64, 96, False, True, us.GATE_SILU)
     full = b.forward().backward().outputs()
