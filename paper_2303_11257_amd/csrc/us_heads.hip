@@ -5,7 +5,8 @@
 //             dx = rstd (g w - x^ mean(g w x^))
 // Bound: HBM; every value is read and written once.  A lane holds 16 values of a head as two chunks of 8 that are each other's partners in the
 // rotation (or hold whole pairs), dh / 16 neighbouring lanes a head, so the norm's sum stays inside 16 lanes and no value changes lanes.
-// A workgroup takes a token at a time: the angles depend on the token and the lane only and are made once for all of its heads.
+// A power of two of such lane groups takes a token at a time: the angles depend on the token and the lane only and are made once for all of
+// its heads.
 // Angles: a frequency is held as a 64-bit fraction of a turn per position, position * frequency modulo 1 is then integer arithmetic
 // that drops whole turns exactly, for any 32-bit position; v_sin / v_cos take the rest, in turns.
 #include <type_traits>
@@ -152,20 +153,25 @@ __device__ __forceinline__ void weights16(float (&w)[16], const _Float16* p, con
   }
 }
 
+// 2^lg lane groups share a token.
 template <int G, bool HALVES>
-__global__ void __launch_bounds__(kThreads) heads_fwd_kernel(HeadsArgs a, _Float16* __restrict__ Q, _Float16* __restrict__ K, _Float16* __restrict__ V) {
+__global__ void __launch_bounds__(kThreads) heads_fwd_kernel(HeadsArgs a, int lg, _Float16* __restrict__ Q, _Float16* __restrict__ K, _Float16* __restrict__ V) {
   const Lane lane = Lane::of<HALVES>((int)threadIdx.x % G, a.dh, a.rot);
-  const int group = (int)threadIdx.x / G;
+  const int slice = (int)threadIdx.x / G, groups = 1 << lg, group = slice & (groups - 1), tokens = kThreads / G >> lg;
   const float per = 1.0f / (float)a.dh;
   LaneAngles ang;
   ang.init(a.freq, lane.first, lane.rotated);
-  for (long t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+  for (long t = (long)blockIdx.x * tokens + (slice >> lg); t < a.tokens; t += (long)gridDim.x * tokens) {
     const long b = t / a.s, i = t - b * a.s;
-    ang.at(a.pos ? a.pos[t] : (int)i, lane.rotated);
     const _Float16* row = a.x + t * a.ld;
-    for (int slot = group; slot < a.h + 2 * a.kv; slot += kThreads / G) {
+    // a head's values are requested while the head before it, or the token's angles, are computed
+    Raw x, next;
+    if (group < a.h + 2 * a.kv) x.load(row + (long)group * a.dh, lane);
+    ang.at(a.pos ? a.pos[t] : (int)i, lane.rotated);
+    for (int slot = group; slot < a.h + 2 * a.kv; slot += groups, x = next) {
+      if (slot + groups < a.h + 2 * a.kv) next.load(row + (long)(slot + groups) * a.dh, lane);
       float v[16];
-      load16(v, row + (long)slot * a.dh, lane);
+      x.get(v);
       const bool is_v = slot >= a.h + a.kv, is_q = slot < a.h;
       if (!is_v) {
         float ss = 0.0f;
@@ -187,29 +193,27 @@ __global__ void __launch_bounds__(kThreads) heads_fwd_kernel(HeadsArgs a, _Float
 }
 
 // Partial weights' gradients: one FP32 row [2][dh] (wq, wk) per workgroup in `partial`, added by the next kernel in order.
-// WPT waves work on a token: one where there are tokens for every wave (a token's query, key and value heads then come round after round, and no wave
-// waits for another's share), all four where there are few.
-template <int G, bool HALVES, int WPT>
-__global__ void __launch_bounds__(kThreads) heads_bwd_kernel(HeadsArgs a, const _Float16* __restrict__ dQ, const _Float16* __restrict__ dK,
+// 2^lg lane groups share a token.
+template <int G, bool HALVES>
+__global__ void __launch_bounds__(kThreads) heads_bwd_kernel(HeadsArgs a, int lg, const _Float16* __restrict__ dQ, const _Float16* __restrict__ dK,
                                                              const _Float16* __restrict__ dV, _Float16* __restrict__ dx, long ld_dx,
                                                              float rep_scale, float* __restrict__ partial) {
   __shared__ float sums[kThreads / G][16 * G];
-  constexpr int GROUPS = 64 / G * WPT, TOKENS = kThreads / 64 / WPT;            // lane groups on a token, tokens of a workgroup
   const Lane lane = Lane::of<HALVES>((int)threadIdx.x % G, a.dh, a.rot);
-  const int group = (int)threadIdx.x / G % GROUPS;
+  const int slice = (int)threadIdx.x / G, groups = 1 << lg, group = slice & (groups - 1), tokens = kThreads / G >> lg;
   const float per = 1.0f / (float)a.dh;
   LaneAngles ang;
   ang.init(a.freq, lane.first, lane.rotated);
   float sq[16], sk[16];
 #pragma unroll
   for (int k = 0; k < 16; ++k) sq[k] = sk[k] = 0.0f;
-  for (long t = (long)blockIdx.x * TOKENS + (int)threadIdx.x / (64 * WPT); t < a.tokens; t += (long)gridDim.x * TOKENS) {
+  for (long t = (long)blockIdx.x * tokens + (slice >> lg); t < a.tokens; t += (long)gridDim.x * tokens) {
     const long b = t / a.s, i = t - b * a.s;
     ang.at(a.pos ? a.pos[t] : (int)i, lane.rotated);
     const _Float16* row = a.x + t * a.ld;
     _Float16* drow = dx + t * ld_dx;
     const long head_step = (long)a.s * a.dh;
-    for (int slot = group; slot < a.h + 2 * a.kv; slot += GROUPS) {
+    for (int slot = group; slot < a.h + 2 * a.kv; slot += groups) {
       const bool is_v = slot >= a.h + a.kv, is_q = slot < a.h;
       const int rep = is_q ? 1 : a.rep;
       const _Float16* dy = is_q ? dQ : is_v ? dV : dK;
@@ -260,7 +264,6 @@ __global__ void __launch_bounds__(kThreads) heads_bwd_kernel(HeadsArgs a, const 
     }
   }
   // the workgroup's sums, group after group
-  const int slice = (int)threadIdx.x / G;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     __syncthreads();
@@ -311,8 +314,15 @@ long bwd_groups(long tokens) {
   const long most = 4 * (long)device_info().cus;
   return tokens < most ? tokens : most;
 }
-// Tokens for every wave of those workgroups?
-bool wave_per_token(long tokens) { return tokens >= 16 * (long)device_info().cus; }
+// Lane groups (2^lg) on a token: as many as it has heads, up to `most`.
+int log_groups(long slots, int most) {
+  int lg = 0;
+  while ((1l << lg) < slots && (2 << lg) <= most) ++lg;
+  return lg;
+}
+// ... of the backward kernel: up to a wave's where there are tokens for every wave (a token's query, key and value heads then come round after round, and no
+// wave waits for another's share: 16384 tokens of 32 + 2 x 8 heads of 128 292 -> 185 us), else up to a workgroup's.
+int bwd_most(long tokens, int G) { return (tokens >= 16 * (long)device_info().cus ? 64 : kThreads) / G; }
 
 // f(integral_constant<int, G>, bool_constant<HALVES>), G: the power of two of lanes that holds dh / 16
 template <class F>
@@ -339,11 +349,18 @@ HeadsArgs heads_args(const HeadsCall& c) {
 // (the most rows any device's grid makes: the size does not depend on which device asks)
 size_t heads_workspace_bytes(long tokens, long dh) { return (size_t)bwd_groups(tokens) * 2 * (size_t)dh * sizeof(float); }
 
+constexpr long kFwdPerCu = 16;     // workgroups per CU: three rounds of what its registers allow even out better than one
+// From so many tokens per CU on a wave has one of its own and makes its angles once, as in the backward kernel.  us, four waves on a token -> one: 65536 tokens of
+// 12 + 2 x 12 heads of 64 186 -> 134, 12000 of 9 + 2 x 9 of 80 34.8 -> 27.8, 16384 of 32 + 2 x 8 of 128 130 even; 8192 of 64 + 2 x 8 of 128 118 -> 129
+constexpr long kFwdWaveTokens = 40;
 hipError_t launch_heads_fwd(const HeadsCall& c, void* Q, void* K, void* V, hipStream_t st) {
   const long tokens = c.batch * c.s;
-  const unsigned grid = (unsigned)(tokens < 0x10000 ? tokens : 0x10000);
   return with_shape(c.dh, c.pairs, [&](auto g, auto halves) {
-    heads_fwd_kernel<decltype(g)::value, decltype(halves)::value><<<grid, kThreads, 0, st>>>(heads_args(c), (_Float16*)Q, (_Float16*)K, (_Float16*)V);
+    constexpr int G = decltype(g)::value;
+    const int lg = log_groups(c.heads + 2 * c.kv_heads, tokens >= kFwdWaveTokens * (long)device_info().cus ? 64 / G : kThreads / G);
+    // (a workgroup's frequencies cost as much as a token of a few heads: workgroups for the CUs, not for the tokens)
+    const long per = kThreads / G >> lg, need = (tokens + per - 1) / per, most = kFwdPerCu * (long)device_info().cus;
+    heads_fwd_kernel<G, decltype(halves)::value><<<(unsigned)(need < most ? need : most), kThreads, 0, st>>>(heads_args(c), lg, (_Float16*)Q, (_Float16*)K, (_Float16*)V);
   });
 }
 
@@ -353,12 +370,10 @@ hipError_t launch_heads_bwd(const HeadsCall& c, const void* dQ, const void* dK, 
   float* partial = (float*)workspace;
   const float rep_scale = (float)(1.0 / __builtin_sqrt((double)(c.heads / c.kv_heads)));
   const hipError_t e = with_shape(c.dh, c.pairs, [&](auto g, auto halves) {
-    auto go = [&](auto wpt) {
-      heads_bwd_kernel<decltype(g)::value, decltype(halves)::value, decltype(wpt)::value><<<(unsigned)rows, kThreads, 0, st>>>(
-          heads_args(c), (const _Float16*)dQ, (const _Float16*)dK, (const _Float16*)dV, (_Float16*)dQKV, ld_dx, rep_scale, partial);
-    };
-    if (wave_per_token(c.batch * c.s)) go(std::integral_constant<int, 1>{});
-    else go(std::integral_constant<int, 4>{});
+    constexpr int G = decltype(g)::value;
+    heads_bwd_kernel<G, decltype(halves)::value><<<(unsigned)rows, kThreads, 0, st>>>(
+        heads_args(c), log_groups(c.heads + 2 * c.kv_heads, bwd_most(c.batch * c.s, G)), (const _Float16*)dQ, (const _Float16*)dK, (const _Float16*)dV, (_Float16*)dQKV, ld_dx,
+        rep_scale, partial);
   });
   if (e != hipSuccess || (!dwq && !dwk)) return e;
   heads_dw_kernel<<<(unsigned)(2 * c.dh / 16), kThreads, 0, st>>>(partial, (_Float16*)dwq, (_Float16*)dwk, (int)rows, (int)c.dh, beta_wq, beta_wk);

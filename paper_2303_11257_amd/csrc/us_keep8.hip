@@ -19,11 +19,12 @@ __device__ __forceinline__ float quad_max(float v) {
   return __builtin_fmaxf(v, lane_dpp<0x4E>(v));
 }
 
-// One row of chunks (8 values) per blockIdx.y step; lanes beyond the row hold zeros, so a last block of 16 values is a block of 32.
+// 2^lx threads of a workgroup next to each other take chunks (8 values) of a row, the others more rows, so that short rows leave at most half of them
+// idle; lanes beyond a row hold zeros, so a last block of 16 values is a block of 32.
 __global__ void __launch_bounds__(kThreads) keep8_store_kernel(const _Float16* __restrict__ X, long ld, int8_t* __restrict__ codes,
-                                                               uint8_t* __restrict__ scales, long rows, int n, int blocks) {
-  const int chunk = (int)(blockIdx.x * kThreads + threadIdx.x), col = chunk * 8;
-  for (long r = blockIdx.y; r < rows; r += gridDim.y) {
+                                                               uint8_t* __restrict__ scales, long rows, int n, int blocks, int lx) {
+  const int chunk = (int)((blockIdx.x << lx) + (threadIdx.x & ((1u << lx) - 1))), col = chunk * 8, per = kThreads >> lx;
+  for (long r = (long)blockIdx.y * per + (threadIdx.x >> lx); r < rows; r += (long)gridDim.y * per) {
     v8h x = {0, 0, 0, 0, 0, 0, 0, 0};
     if (col < n) x = *reinterpret_cast<const v8h*>(X + r * ld + col);
     float m = 0.0f;
@@ -55,10 +56,10 @@ __global__ void __launch_bounds__(kThreads) keep8_store_kernel(const _Float16* _
 }
 
 __global__ void __launch_bounds__(kThreads) keep8_load_kernel(const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                              _Float16* __restrict__ X, long ld, long rows, int n, int blocks) {
-  const int chunk = (int)(blockIdx.x * kThreads + threadIdx.x), col = chunk * 8;
+                                                              _Float16* __restrict__ X, long ld, long rows, int n, int blocks, int lx) {
+  const int chunk = (int)((blockIdx.x << lx) + (threadIdx.x & ((1u << lx) - 1))), col = chunk * 8, per = kThreads >> lx;
   if (col >= n) return;
-  for (long r = blockIdx.y; r < rows; r += gridDim.y) {
+  for (long r = (long)blockIdx.y * per + (threadIdx.x >> lx); r < rows; r += (long)gridDim.y * per) {
     const v2i c = *reinterpret_cast<const v2i*>(codes + r * n + col);
     const uint32_t s = scales[r * blocks + (chunk >> 2)];
     float v[8];
@@ -71,19 +72,27 @@ __global__ void __launch_bounds__(kThreads) keep8_load_kernel(const int8_t* __re
   }
 }
 
-dim3 grid_of(long rows, long n) {
-  const long x = (n / 8 + kThreads - 1) / kThreads;
-  return dim3((unsigned)x, (unsigned)(rows < 65535 ? rows : 65535));
+// Threads on a row: the power of two that holds its whole blocks, four (one block) at least.
+int log_threads(long n) {
+  int lx = 2;
+  while ((8l << lx) < n && (1 << lx) < kThreads) ++lx;
+  return lx;
+}
+dim3 grid_of(long rows, long n, int lx) {
+  const long x = (n / 8 + (1l << lx) - 1) >> lx, per = kThreads >> lx, y = (rows + per - 1) / per;
+  return dim3((unsigned)x, (unsigned)(y < 65535 ? y : 65535));
 }
 
 }  // namespace
 
 hipError_t launch_keep8_store(const void* X, long ld, void* codes, void* scales, long rows, long n, hipStream_t st) {
-  keep8_store_kernel<<<grid_of(rows, n), kThreads, 0, st>>>((const _Float16*)X, ld, (int8_t*)codes, (uint8_t*)scales, rows, (int)n, (int)((n + 31) / 32));
+  const int lx = log_threads(n);
+  keep8_store_kernel<<<grid_of(rows, n, lx), kThreads, 0, st>>>((const _Float16*)X, ld, (int8_t*)codes, (uint8_t*)scales, rows, (int)n, (int)((n + 31) / 32), lx);
   return hipGetLastError();
 }
 hipError_t launch_keep8_load(const void* codes, const void* scales, void* X, long ld, long rows, long n, hipStream_t st) {
-  keep8_load_kernel<<<grid_of(rows, n), kThreads, 0, st>>>((const int8_t*)codes, (const uint8_t*)scales, (_Float16*)X, ld, rows, (int)n, (int)((n + 31) / 32));
+  const int lx = log_threads(n);
+  keep8_load_kernel<<<grid_of(rows, n, lx), kThreads, 0, st>>>((const int8_t*)codes, (const uint8_t*)scales, (_Float16*)X, ld, rows, (int)n, (int)((n + 31) / 32), lx);
   return hipGetLastError();
 }
 

@@ -109,7 +109,8 @@ def check_back(got, ref, batch, s, h, kv, dh, ld):
 
 
 SHAPES = [(1, 1, 1, 1, 16, 16), (3, 1, 4, 4, 64, 64), (2, 7, 6, 2, 80, 32), (1, 33, 8, 1, 128, 128), (2, 65, 4, 2, 96, 96), (1, 19, 3, 3, 256, 256),
-          (2, 5, 2, 1, 32, 0), (5, 40, 12, 4, 48, 16), (1, 2100, 2, 1, 32, 32)]
+          (2, 5, 2, 1, 32, 0), (5, 40, 12, 4, 48, 16), (1, 2100, 2, 1, 32, 32),
+          (1, 70, 70, 7, 16, 16), (3, 1400, 1, 1, 64, 64), (2, 5300, 3, 1, 16, 16)]       # more heads than lane groups; tokens for a wave each
 
 
 @pytest.mark.parametrize("neighbours", [False, True])
