@@ -450,7 +450,8 @@ us_status us_sum_bwd(const void* G, void* dX, long rows, long n, float beta, voi
  *   scratch that this call fills again from the kept values with the factor alpha (the forward call's H need not live until then).
  *   With T = 0 the weights' gradients are zeros.
  * Workspace (16-byte aligned, contents undefined on entry and exit): us_ffn_gated_workspace_bytes serves both; the forward call can do
- * without (NULL), the backward call needs it where a weight's gradient is cut into slices, as us_linear_bwd does.
+ * without (NULL; up to 64 tokens it is then slower and adds in another order), the backward call needs it where a weight's gradient is cut into
+ * slices, as us_linear_bwd does.  Calls that may overlap on a GPU need a workspace each.
  * Outputs must not overlap inputs or one another.  A gate outside the list is US_ERR_DTYPE, an unknown mode bit US_ERR_VALUE.
  */
 typedef enum { US_GATE_SILU = 0, US_GATE_GELU = 1, US_GATE_RELU = 2, US_GATE_SIGMOID = 3 } us_gate;

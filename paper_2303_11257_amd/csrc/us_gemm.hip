@@ -129,17 +129,17 @@ hipError_t gemm_gate_three_f16(const GemmProblem& dx, const GemmProblem& dwgu, c
 hipError_t gemm_gate_three_fp8(const GemmProblem& dx, const GemmProblem& dwgu, const GemmProblem& dwd, hipStream_t st);
 
 // All three products of the gated block behind dZ in one launch: where all are few tiles (two launches fall away: FP16 64 x 256 x 688 backward call 14.4 -> 11.6 us),
-// or on 128 x 128 tiles, two workgroups per CU, where the longest tile takes at most two and a half times a workgroup's share of the work and none of
+// or on 128 x 128 tiles, two workgroups per CU, where the longest tile takes half to two and a half times a workgroup's share of the work and none of
 // them makes large tiles for all CUs.  Backward call, two or three launches with K slices -> one: FP16 4096 x 768 x 2048 112.8 -> 87.6, FP8 3000 x 768 x 2048
-// 65.4 -> 41.8, 1024 x 2048 x 5632 106 -> 95; over 34 drawn blocks that the rule takes the geometric mean is 0.85 (one slower, FP16 6189 x 1360 x 2720 by
-// 2 %).  Beyond it: longest / share = 3.2 FP16 1024 x 1024 x 2048 54.9 -> 58.2, FP8 1024 x 1024 x 2736 50.5 -> 55.4, 9 FP8 16000 x 256 x 688 81 -> 124.
+// 65.4 -> 41.8, 1024 x 2048 x 5632 106 -> 95; over 32 drawn blocks that the rule takes the geometric mean is 0.85, none slower.
+//  Outside: longest / share = 0.4 FP8 8192 x 1024 x 4096 233.9 -> 233.4, FP16 6189 x 1360 x 2720 352 -> 359; 3.2 FP16 1024 x 1024 x 2048 54.9 -> 58.2, FP8 1024 x 1024 x 2736 50.5 -> 55.4, 9 FP8 16000 x 256 x 688 81 -> 124.
 bool gemm_gate_three_ok(const GemmProblem& dx, const GemmProblem& dwgu, const GemmProblem& dwd) {
   if (!offsets_fit(dx) || !offsets_fit(dwgu) || !offsets_fit(dwd)) return false;
   if (small_tile_choice(dx) != SmallTileChoice::None && small_tile_choice(dwgu) != SmallTileChoice::None && small_tile_choice(dwd) != SmallTileChoice::None) return true;
   if (use_big_tile(dx.M, dx.N, 1) || use_big_tile(dwgu.M, dwgu.N, 1) || use_big_tile(dwd.M, dwd.N, 1)) return false;
   auto tiles = [](const GemmProblem& p) { return ceil_div(p.M, 128) * ceil_div(p.N, 128); };
   const long work = tiles(dx) * dx.K + (tiles(dwgu) + tiles(dwd)) * dwd.K, longest = dx.K > dwd.K ? dx.K : dwd.K;
-  return 4 * cu_count() * longest <= 5 * work;
+  return 4 * cu_count() * longest >= work && 4 * cu_count() * longest <= 5 * work;
 }
 hipError_t gemm_gate_three(const GemmProblem& dx, const GemmProblem& dwgu, const GemmProblem& dwd, hipStream_t st) {
   return dx.a_dt == US_F16 ? gemm_gate_three_f16(dx, dwgu, dwd, st) : gemm_gate_three_fp8(dx, dwgu, dwd, st);

@@ -84,6 +84,7 @@ def test_nothing_to_do_is_no_error():
 
 def test_sizes_and_factors():
     assert [us.keep8_blocks(n) for n in (-3, 0, 1, 32, 33, 4096)] == [0, 0, 1, 1, 2, 128]
+    assert [us.lib().us_keep8_blocks(n) for n in (-3, 0, 1, 32, 33, 4096)] == [0, 0, 1, 1, 2, 128]
     assert us.ffn_gated_workspace_bytes(0, 16, 16) == 0 and us.qk_norm_rope_workspace_bytes(1, 0, 1, 1, 16) == 0
     assert us.ffn_gated_workspace_bytes(4096, 512, 2048) >= us.workspace_bytes(4096, 512, 4096)
     assert us.ffn_gated_workspace_bytes(4096, 512, 2048) >= us.workspace_bytes(4096, 2048, 512)
