@@ -79,9 +79,10 @@ __device__ __forceinline__ float row_max_across(float own, bool ignore_nan) {
   return f(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
-// Codes of a row's share of a block, NQ quads of a lane, and the block's scale.
+// Codes of a row's share of a block, NQ quads of a lane, and the block's scale.  half_block: its last 16 columns, the second half of a lane's quads, do not
+// exist; their sums are zero, but NaN in a row of X with an infinity, which must not mark the block.
 template <bool M16, int NQ>
-__device__ __forceinline__ uint32_t keep_quads(const v4f (&z)[NQ], int (&code)[NQ]) {
+__device__ __forceinline__ uint32_t keep_quads(const v4f (&z)[NQ], int (&code)[NQ], bool half_block) {
   float m = 0.0f;
 #pragma unroll
   for (int q = 0; q < NQ; ++q)
@@ -102,7 +103,7 @@ __device__ __forceinline__ uint32_t keep_quads(const v4f (&z)[NQ], int (&code)[N
     for (int q = 0; q < NQ; ++q) {
       code[q] = keep_codes_any(z[q][0], z[q][1], z[q][2], z[q][3], keep_inverse(s));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) nan |= z[q][e] != z[q][e];
+      for (int e = 0; e < 4; ++e) nan |= z[q][e] != z[q][e] && !(half_block && q >= NQ / 2);
     }
     return s + (row_max_across<M16>(nan ? 1.0f : 0.0f, true) != 0.0f ? kKeepNan : 0);
   }
@@ -178,7 +179,8 @@ __device__ __forceinline__ void gate_epilogue(const GemmArgs& g, const Acc& acc,
           }
           if constexpr (KEEP8) {
             int cg[NQ], cu[NQ];
-            const uint32_t sg = keep_quads<M16>(zg, cg), su = keep_quads<M16>(zu, cu);
+            const bool half_block = cols - j * 32 == 16;
+            const uint32_t sg = keep_quads<M16>(zg, cg, half_block), su = keep_quads<M16>(zu, cu, half_block);
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
               const int col = j * 32 + Acc::col(h * NQ + q, lane);
@@ -407,7 +409,7 @@ __device__ __forceinline__ void gate_point(const GemmArgs& g, long m, long n, bo
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         big = __builtin_fmaxf(big, __builtin_fabsf(z[k]));
-        rare |= z[k] != z[k];
+        rare |= in && z[k] != z[k];          // (columns beyond the matrix: NaN in a row of X with an infinity)
       }
       big = __builtin_fmaxf(big, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, big), 0xB1, 0xf, 0xf, true)));
       big = __builtin_fmaxf(big, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, big), 0x4E, 0xf, 0xf, true)));

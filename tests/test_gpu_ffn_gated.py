@@ -274,6 +274,18 @@ def test_infinities_and_nan_stay_in_their_rows(T):
             assert torch.isnan(dirty["Z"][1]).all() and torch.isinf(dirty["Z"][2]).all()
 
 
+@pytest.mark.parametrize("T,f", [(3, 80), (9, 4112), (300, 1040), (700, 2064), (3000, 4112)])
+def test_an_infinity_marks_no_block(T, f):
+    """An infinite X makes infinities, which are clipped; the columns that a last block of 16 lacks are NaN on the way and must not show."""
+    b = Block(T, 1024 if T == 9 else 64, f, False, True, us.GATE_SILU)
+    b.g["X"][2, 9] = float("inf")
+    b.forward()
+    out = b.outputs()
+    assert (out["Z"][2].abs() == 127).all() and (out["Zs"][2] == 136).all()
+    rest = [r for r in range(T) if r != 2]
+    assert (out["Zs"][rest] <= 136).all()
+
+
 def test_gradients_against_differences():
     """With one factor for both halves of dZ the gradients are those of <Y, G> up to known factors: dX (2f)^1/2 (f/d)^-1/2 ... all products' factors
     divided out.  Central difference in 64 bits along a direction v, step 2^-8: its error, h^2 / 6 times a third derivative of order one per
