@@ -161,7 +161,8 @@ def check_backward(b, out, alpha=None, beta_gate=None, beta_up=None):
 
 
 # one token, a few, odd numbers; widths that end inside a block of 32, a tile's half and a tile; all kernels' tiles
-SHAPES = [(1, 16, 16), (1, 256, 688), (5, 48, 32), (33, 64, 80), (64, 528, 144), (65, 512, 2064), (130, 256, 272), (600, 512, 1040), (1999, 272, 528), (2048, 128, 2064), (1300, 64, 4112)]
+SHAPES = [(1, 16, 16), (1, 256, 688), (5, 48, 32), (33, 64, 80), (64, 528, 144), (65, 512, 2064), (130, 256, 272), (600, 512, 1040), (1999, 272, 528), (2048, 128, 2064), (1300, 64, 4112),
+          (4095, 256, 4112), (5001, 128, 272)]            # an odd number of tokens as reduction: of wave groups in one launch, and in slices
 
 
 @pytest.mark.parametrize("keep8", [False, True])
@@ -175,6 +176,10 @@ def test_forward_and_backward(T, d, f, fp8, keep8):
     if keep8:
         b.H.view(torch.uint8)[: b.T].fill_(0x3c)             # the forward call's H is not read again
     b.backward()
+    if T == 4095:
+        assert "pair:" in us.last_launch() or fp8, us.last_launch()
+    if T == 5001:
+        assert "partial" in us.last_launch(), us.last_launch()
     out = b.outputs()
     assert torch.equal(out["Z"], first["Z"])
     check_backward(b, out)
