@@ -4,8 +4,9 @@
 //   backward  g = R^-1(dy) (K, V: the sharing heads' gradients added in FP32, times repeats^-1/2);  dw = beta sum g x^;
 //             dx = rstd (g w - x^ mean(g w x^))
 // Bound: HBM; every value is read and written once: 16384 tokens of 32 query and 2 x 8 shared heads of 128, forward 604 MB in 118 us = 5.1 TB/s (a large copy: 5.1),
-// backward 805 MB in 184 us = 4.4, bound by two waves per SIMD (the weights' sums and the angles stay in registers; held to three or four, the
-// compiler spills: 208 and 323 us).  Heads of 64 and 96 have half of the bytes per angle: forward 4.5 and 3.0 TB/s.  A lane holds 16 values of a head as two chunks of 8 that are each other's partners in the
+// backward 805 MB in 178 us = 4.5, bound by two waves per SIMD (in heads above 64 the weights' sums and the angles stay in registers; held to three or
+// four, the compiler spills: 208 and 323 us).  Heads of 64 and 96 have half of the bytes per angle: forward 4.5 and 3.0 TB/s,
+// backward 4.2 (three waves) and 3.1.  A lane holds 16 values of a head as two chunks of 8 that are each other's partners in the
 // rotation (or hold whole pairs), dh / 16 neighbouring lanes a head, so the norm's sum stays inside 16 lanes and no value changes lanes.
 // A power of two of such lane groups takes a token at a time: the angles depend on the token and the lane only and are made once for all of
 // its heads.
@@ -200,15 +201,24 @@ template <int G, bool HALVES>
 __global__ void __launch_bounds__(kThreads) heads_bwd_kernel(HeadsArgs a, int lg, const _Float16* __restrict__ dQ, const _Float16* __restrict__ dK,
                                                              const _Float16* __restrict__ dV, _Float16* __restrict__ dx, long ld_dx,
                                                              float rep_scale, float* __restrict__ partial) {
-  __shared__ float sums[kThreads / G][16 * G];
+  // The weights' sums over a lane group's heads and tokens, added up in program order.  Heads of up to 64 keep them in LDS, which leaves registers for a third
+  // wave per SIMD; wider heads keep them in registers, as their rounds wait for memory and not for each other (registers -> LDS, us: 16384 tokens of
+  // 2 + 2 x 1 heads of 32 20.4 -> 14.5, 65536 of 12 + 2 x 12 of 64 275 -> 262, 16384 of 32 + 2 x 8 of 128 185 -> 189, 16384 of 16 + 2 x 2 of 256 170 -> 177).
+  constexpr bool kInLds = G <= 4;
+  __shared__ __attribute__((aligned(16))) float sums[kInLds ? 2 : 1][kThreads / G][16 * G];
   const Lane lane = Lane::of<HALVES>((int)threadIdx.x % G, a.dh, a.rot);
   const int slice = (int)threadIdx.x / G, groups = 1 << lg, group = slice & (groups - 1), tokens = kThreads / G >> lg;
   const float per = 1.0f / (float)a.dh;
   LaneAngles ang;
   ang.init(a.freq, lane.first, lane.rotated);
   float sq[16], sk[16];
+  if constexpr (kInLds) {
+    for (int c = (int)threadIdx.x; c < 2 * kThreads * 16; c += kThreads) (&sums[0][0][0])[c] = 0.0f;
+    __syncthreads();
+  } else {
 #pragma unroll
-  for (int k = 0; k < 16; ++k) sq[k] = sk[k] = 0.0f;
+    for (int k = 0; k < 16; ++k) sq[k] = sk[k] = 0.0f;
+  }
   for (long t = (long)blockIdx.x * tokens + (slice >> lg); t < a.tokens; t += (long)gridDim.x * tokens) {
     const long b = t / a.s, i = t - b * a.s;
     ang.at(a.pos ? a.pos[t] : (int)i, lane.rotated);
@@ -249,14 +259,33 @@ __global__ void __launch_bounds__(kThreads) heads_bwd_kernel(HeadsArgs a, int lg
         for (int k = 0; k < 16; ++k) ss = __builtin_fmaf(v[k], v[k], ss);
         const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(head_sum<G>(ss), per, a.eps));
         float dot = 0.0f;
+        if constexpr (kInLds) {
+          float* const mine = sums[is_q ? 0 : 1][slice];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          v[k] *= rstd;
-          const float gv = g[k] * v[k];
-          sq[k] += is_q ? gv : 0.0f;
-          sk[k] += is_q ? 0.0f : gv;
-          g[k] *= w[k];
-          dot = __builtin_fmaf(g[k], v[k], dot);
+          for (int q = 0; q < 4; ++q) {
+            v4f* const at = reinterpret_cast<v4f*>(mine + (q < 2 ? lane.a : lane.b - 8) + 4 * q);
+            v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (lane.on) s = *at;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int k = 4 * q + e;
+              v[k] *= rstd;
+              s[e] += g[k] * v[k];
+              g[k] *= w[k];
+              dot = __builtin_fmaf(g[k], v[k], dot);
+            }
+            if (lane.on) *at = s;
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            v[k] *= rstd;
+            const float gv = g[k] * v[k];
+            sq[k] += is_q ? gv : 0.0f;
+            sk[k] += is_q ? 0.0f : gv;
+            g[k] *= w[k];
+            dot = __builtin_fmaf(g[k], v[k], dot);
+          }
         }
         dot = head_sum<G>(dot) * per;
 #pragma unroll
@@ -269,17 +298,19 @@ __global__ void __launch_bounds__(kThreads) heads_bwd_kernel(HeadsArgs a, int lg
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     __syncthreads();
-    if (lane.on) {
+    if constexpr (!kInLds) {
+      if (lane.on) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        sums[slice][lane.a + k] = which ? sk[k] : sq[k];
-        sums[slice][lane.b + k] = which ? sk[k + 8] : sq[k + 8];
+        for (int k = 0; k < 8; ++k) {
+          sums[0][slice][lane.a + k] = which ? sk[k] : sq[k];
+          sums[0][slice][lane.b + k] = which ? sk[k + 8] : sq[k + 8];
+        }
       }
+      __syncthreads();
     }
-    __syncthreads();
     for (int c = (int)threadIdx.x; c < a.dh; c += kThreads) {
       float s = 0.0f;
-      for (int q = 0; q < kThreads / G; ++q) s += sums[q][c];
+      for (int q = 0; q < kThreads / G; ++q) s += sums[kInLds ? which : 0][q][c];
       partial[((long)blockIdx.x * 2 + which) * a.dh + c] = s;
     }
   }
@@ -311,9 +342,11 @@ __global__ void __launch_bounds__(kThreads) heads_dw_kernel(const float* __restr
   }
 }
 
-// Workgroups of the backward kernel: four per CU, which is what its registers allow, or one per token.
-long bwd_groups(long tokens) {
-  const long most = 4 * (long)device_info().cus;
+// Workgroups of the backward kernel: one per wave that its registers leave a SIMD, so that all run at once and each makes its frequencies and its row of sums once
+// (us, four per CU -> this: 65536 tokens of 12 + 2 x 12 heads of 64 264 -> 216, 16384 of 1 + 2 x 1 of 64 17.0 -> 13.3, 16384 of 32 + 2 x 8 of 128
+// 185 -> 178), or one per token.
+long bwd_groups(long tokens, long dh) {
+  const long most = (dh <= 64 ? 3 : 2) * (long)device_info().cus;
   return tokens < most ? tokens : most;
 }
 // Lane groups (2^lg) on a token: as many as it has heads, up to `most`.
@@ -349,7 +382,7 @@ HeadsArgs heads_args(const HeadsCall& c) {
 }  // namespace
 
 // (the most rows any device's grid makes: the size does not depend on which device asks)
-size_t heads_workspace_bytes(long tokens, long dh) { return (size_t)bwd_groups(tokens) * 2 * (size_t)dh * sizeof(float); }
+size_t heads_workspace_bytes(long tokens, long dh) { return (size_t)bwd_groups(tokens, dh) * 2 * (size_t)dh * sizeof(float); }
 
 constexpr long kFwdPerCu = 16;     // workgroups per CU: three rounds of what its registers allow even out better than one
 // From so many tokens per CU on a wave has one of its own and makes its angles once, as in the backward kernel.  us, four waves on a token -> one: 65536 tokens of
@@ -368,7 +401,7 @@ hipError_t launch_heads_fwd(const HeadsCall& c, void* Q, void* K, void* V, hipSt
 
 hipError_t launch_heads_bwd(const HeadsCall& c, const void* dQ, const void* dK, const void* dV, void* dQKV, long ld_dx, void* dwq, void* dwk,
                             float beta_wq, float beta_wk, void* workspace, hipStream_t st) {
-  const long rows = bwd_groups(c.batch * c.s);
+  const long rows = bwd_groups(c.batch * c.s, c.dh);
   float* partial = (float*)workspace;
   const float rep_scale = (float)(1.0 / __builtin_sqrt((double)(c.heads / c.kv_heads)));
   const hipError_t e = with_shape(c.dh, c.pairs, [&](auto g, auto halves) {
