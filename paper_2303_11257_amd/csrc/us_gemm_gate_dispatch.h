@@ -11,29 +11,39 @@ namespace us {
 //         4096 x 768 x 2048 48.6 -> 50.2, 2048 x 4096 x 8192 347 -> 344
 using CfgG256 = GemmCfg<256, 256, 4, 2, 128, 2, 1>;
 
+// FP8 products of at most so many tokens go to the matrix core as FP16.  H and dZ are rounded to codes an eighth and a quarter wide: where the FP8 adder moves a
+// code of dZ across a border, a column of dWgu = T^-1/2 X^T dZ moves by step * X * T^-1/2, which few tokens do not average out (14 to 409 tokens of d = 1072 to
+// 2816: single elements off by up to half of the RMS; from 1216 on by 0.2 and less).
+constexpr long kAsF16Rows = 1024;
+
 // EPI: of the forward product (NN) or of dH (NT).
-template <bool FP8, bool NT, int EPI>
+template <bool FP8, bool NT, int EPI, bool AS_F16 = false>
 hipError_t launch_gate(const GemmProblem& p, hipStream_t st) {
-  constexpr int FA = FP8 && NT ? 1 : 0;                // dH: G is E5M2
+  constexpr int FB = AS_F16 ? kAsF16 : 0, FA = FB + (FP8 && NT ? 1 : 0);      // dH: G is E5M2
   if (!offsets_fit(p)) return hipErrorInvalidValue;
+  if constexpr (FP8 && !AS_F16) {
+    if (p.M <= kAsF16Rows) return launch_gate<FP8, NT, EPI, true>(p, st);
+  }
   const SmallTileChoice c = small_tile_choice(p);
-  if (c == SmallTileChoice::T32x32 || c == SmallTileChoice::T32x64 || (c == SmallTileChoice::None && p.M <= 32)) return launch_small<CfgT32x64, FP8, FA, 0, true, NT, EPI, false>(p, st);
-  if (c == SmallTileChoice::T64x64) return launch_small<CfgT64x64, FP8, FA, 0, true, NT, EPI, false>(p, st);
-  using Big = typename std::conditional<!NT && (FP8 || EPI == EPI_GATE8), CfgG256, CfgD256>::type;
-  // dH with Z in FP16 and a short reduction: two workgroups per CU, one of which reads its Z and stores its dZ under the other's products, where large
-  // tiles all read at once.  us, dZ alone, D256 -> D128: FP8 8192 x K x 4096, K = 512 72.1 -> 52.8, 1024 82.1 -> 64.8, 2048 100 -> 89, 2560 115 -> 108,
-  // 4096 x 4096 x 4096 71.5 -> 74.4; FP16 K = 512 96 -> 75, 1024 111 -> 109, 2048 161 -> 162; with 8-bit blocks, half of the bytes, FP8 K = 512 54.5 -> 56.1,
-  // 1024 64.6 -> 68.9, FP16 1024 98 -> 108: not taken
-  const bool two_per_cu = EPI == EPI_GATE_GRAD && p.K * (FP8 ? 1 : 2) <= 2560;
-  // one round of large tiles instead of two of small ones, as for the layers' products: us, forward call, D128 -> large, FP16 1999 x 1552 x 2064 78.1 -> 63.1,
-  // FP8 50.0 -> 40.6, 2300 x 2048 x 2048 49.1 -> 41.8
-  if (use_big_single(p, false) && !two_per_cu) return launch_one<true, Big, FP8, FA, 0, true, NT, EPI, false>(p, 1, p.K, st);
-  // Tiles that give every CU at most one, and a reduction of 2048 bytes or more: two wave groups.  us, forward call / dZ, D128 -> W128: FP16 512 x 4096 x 4096
-  // 74.2 / 44.5 -> 64.6 / 31.0, 1024 x 1024 x 1376 24.4 / 12.2 -> 22.1 / 12.0, FP8 1024 x 2048 x 2048 29.3 / 13.0 -> 27.7 / 13.1; shorter: FP8 1024 x 1024 x 1376
-  // 17.0 / 11.3 -> 17.5 / 11.3, FP16 1024 x 512 x 1376 15.9 / 9.3 -> 16.5 / 9.7
-  if (ceil_div(p.M, 128) * ceil_div(p.N, 128) <= cu_count() && p.K * (FP8 ? 1 : 2) >= 2048)
-    return launch_one<true, CfgW128, FP8, FA, 0, true, NT, EPI, false>(p, 1, p.K, st);
-  return launch_one<true, CfgD128, FP8, FA, 0, true, NT, EPI, false>(p, 1, p.K, st);
+  if (c == SmallTileChoice::T32x32 || c == SmallTileChoice::T32x64 || (c == SmallTileChoice::None && p.M <= 32)) return launch_small<CfgT32x64, FP8, FA, FB, true, NT, EPI, false>(p, st);
+  if (c == SmallTileChoice::T64x64) return launch_small<CfgT64x64, FP8, FA, FB, true, NT, EPI, false>(p, st);
+  if constexpr (!AS_F16) {                             // (fragments of larger tiles do not fit the registers as FP16)
+    using Big = typename std::conditional<!NT && (FP8 || EPI == EPI_GATE8), CfgG256, CfgD256>::type;
+    // dH with Z in FP16 and a short reduction: two workgroups per CU, one of which reads its Z and stores its dZ under the other's products, where large
+    // tiles all read at once.  us, dZ alone, D256 -> D128: FP8 8192 x K x 4096, K = 512 72.1 -> 52.8, 1024 82.1 -> 64.8, 2048 100 -> 89, 2560 115 -> 108,
+    // 4096 x 4096 x 4096 71.5 -> 74.4; FP16 K = 512 96 -> 75, 1024 111 -> 109, 2048 161 -> 162; with 8-bit blocks, half of the bytes, FP8 K = 512 54.5 -> 56.1,
+    // 1024 64.6 -> 68.9, FP16 1024 98 -> 108: not taken
+    const bool two_per_cu = EPI == EPI_GATE_GRAD && p.K * (FP8 ? 1 : 2) <= 2560;
+    // one round of large tiles instead of two of small ones, as for the layers' products: us, forward call, D128 -> large, FP16 1999 x 1552 x 2064 78.1 -> 63.1,
+    // FP8 50.0 -> 40.6, 2300 x 2048 x 2048 49.1 -> 41.8
+    if (use_big_single(p, false) && !two_per_cu) return launch_one<true, Big, FP8, FA, FB, true, NT, EPI, false>(p, 1, p.K, st);
+    // Tiles that give every CU at most one, and a reduction of 2048 bytes or more: two wave groups.  us, forward call / dZ, D128 -> W128: FP16 512 x 4096 x 4096
+    // 74.2 / 44.5 -> 64.6 / 31.0, 1024 x 1024 x 1376 24.4 / 12.2 -> 22.1 / 12.0, FP8 1024 x 2048 x 2048 29.3 / 13.0 -> 27.7 / 13.1; shorter: FP8 1024 x 1024 x 1376
+    // 17.0 / 11.3 -> 17.5 / 11.3, FP16 1024 x 512 x 1376 15.9 / 9.3 -> 16.5 / 9.7
+    if (ceil_div(p.M, 128) * ceil_div(p.N, 128) <= cu_count() && p.K * (FP8 ? 1 : 2) >= 2048)
+      return launch_one<true, CfgW128, FP8, FA, FB, true, NT, EPI, false>(p, 1, p.K, st);
+  }
+  return launch_one<true, CfgD128, FP8, FA, FB, true, NT, EPI, false>(p, 1, p.K, st);
 }
 
 // The three products behind dZ in one launch, the one with the longest tiles first: dX = dZ Wgu^T (NT), dWgu = X^T dZ and dWd = H^T G (TN), plain results.  Their

@@ -312,11 +312,11 @@ hipError_t launch_rows_ffn(const GemmProblem& up, const GemmProblem& down, bool 
   return launch_store_of_sums(down, partial, slices, st);
 }
 
-// A product on the few-tiles kernel with its reduction in slices, FP32 sums.
-template <class Cfg, bool FP8>
+// A product on the few-tiles kernel with its reduction in slices, FP32 sums.  F: formats (the gate's sums as FP16, as in launch_gate).
+template <class Cfg, bool FP8, int F>
 hipError_t launch_small_slices(const GemmProblem& p, int slices, float* partial, hipStream_t st) {
   constexpr int LDS = SmallTile<Cfg, FP8, true, false>::LDS_BYTES;
-  auto kern = gemm_small_kernel<Cfg, FP8, 0, 0, true, false, EPI_PARTIAL, true>;
+  auto kern = gemm_small_kernel<Cfg, FP8, F, F, true, false, EPI_PARTIAL, true>;
   note_gemm_launch("direct", Cfg::BM, Cfg::BN, Cfg::WAVES, Cfg::NST, FP8, true, false, EPI_PARTIAL, true, slices);
   static FuncConfig cfg;
   if (hipError_t e = cfg.ensure((const void*)kern, LDS); e != hipSuccess) return e;
@@ -334,13 +334,13 @@ hipError_t gemm_rows_ffn(const GemmProblem& up, const GemmProblem& down, bool ke
 
 hipError_t gemm_small_gate(const GemmProblem& up, int slices, bool keep8, void* partial, hipStream_t st) {
   const bool fp8 = up.a_dt != US_F16;
-  const hipError_t e = fp8 ? launch_small_slices<CfgT32x64, true>(up, slices, (float*)partial, st) : launch_small_slices<CfgT32x64, false>(up, slices, (float*)partial, st);
+  const hipError_t e = fp8 ? launch_small_slices<CfgT32x64, true, kAsF16>(up, slices, (float*)partial, st) : launch_small_slices<CfgT32x64, false, 0>(up, slices, (float*)partial, st);
   if (e != hipSuccess) return e;
   return fp8 ? launch_gate_of_sums<true>(up, keep8, (const float*)partial, slices, st) : launch_gate_of_sums<false>(up, keep8, (const float*)partial, slices, st);
 }
 hipError_t gemm_small_store(const GemmProblem& down, int slices, void* partial, hipStream_t st) {
-  const hipError_t e = down.a_dt != US_F16 ? launch_small_slices<CfgT32x32, true>(down, slices, (float*)partial, st)
-                                           : launch_small_slices<CfgT32x32, false>(down, slices, (float*)partial, st);
+  const hipError_t e = down.a_dt != US_F16 ? launch_small_slices<CfgT32x32, true, 0>(down, slices, (float*)partial, st)
+                                           : launch_small_slices<CfgT32x32, false, 0>(down, slices, (float*)partial, st);
   return e != hipSuccess ? e : launch_store_of_sums(down, (const float*)partial, slices, st);
 }
 
