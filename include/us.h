@@ -436,7 +436,8 @@ us_status us_sum_bwd(const void* G, void* dX, long rows, long n, float beta, voi
  * us_ffn_gated_fwd:  Z[T,2f] = d^-1/2 X Wgu = [Zg | Zu];  H[T,f] = alpha f(Zg) Zu;  Y[T,d] = fp16(f^-1/2 H Wd)      alpha <= 0: us_gate_scales'
  *   X [T,d], Wgu [d,2f] (the gate's columns first), Wd [f,d]; T is free (one token upwards, no multiple of anything), d and f are
  *   multiples of 16 from 16 to US_FFN_GATED_MAX.
- *   mode: US_FFN_FP8: operands are E4M3 codes (else FP16) and H receives E4M3 codes (else FP16).
+ *   mode: US_FFN_FP8: operands are E4M3 codes (else FP16) and H receives E4M3 codes (else FP16).  Z's and dH's sums are FP32 sums of exact products for
+ *   up to 1024 tokens, the matrix core's FP8 sums (1.3e-5 rms of a unit off) for more.
  *   H is made from the FP32 sums and rounded once.  Z is what the backward pass needs: FP16, or with US_FFN_KEEP8 8-bit blocks (us_keep8_store's
  *   format, also made from the FP32 sums, the blocks of Zg and of Zu starting at their first columns): codes Z [T,2f] and scales Zs
  *   [T, 2 us_keep8_blocks(f)].  Without US_FFN_KEEP8 Zs is not used and Z may be NULL: nothing is kept (serving).

@@ -13,7 +13,8 @@ using CfgG256 = GemmCfg<256, 256, 4, 2, 128, 2, 1>;
 
 // FP8 products of at most so many tokens go to the matrix core as FP16.  H and dZ are rounded to codes an eighth and a quarter wide: where the FP8 adder moves a
 // code of dZ across a border, a column of dWgu = T^-1/2 X^T dZ moves by step * X * T^-1/2, which few tokens do not average out (14 to 409 tokens of d = 1072 to
-// 2816: single elements off by up to half of the RMS; from 1216 on by 0.2 and less).
+// 2816: single elements off by up to half of the RMS, as FP16 by 0.01; from 1216 on by 0.2 and less).  It costs, us, FP8 -> FP16: forward and backward 14 x 1072 x 2848
+// 45.9 -> 46.1, 409 x 1920 x 7680 158 -> 171, 1024 x 4096 x 11008 621 -> 685; forward 16 x 2048 x 5632 23.5 -> 23.3, 512 x 4096 x 11008 88 -> 131.
 constexpr long kAsF16Rows = 1024;
 
 // EPI: of the forward product (NN) or of dH (NT).
@@ -38,7 +39,7 @@ hipError_t launch_gate(const GemmProblem& p, hipStream_t st) {
     // FP8 50.0 -> 40.6, 2300 x 2048 x 2048 49.1 -> 41.8
     if (use_big_single(p, false) && !two_per_cu) return launch_one<true, Big, FP8, FA, FB, true, NT, EPI, false>(p, 1, p.K, st);
     // Tiles that give every CU at most one, and a reduction of 2048 bytes or more: two wave groups.  us, forward call / dZ, D128 -> W128: FP16 512 x 4096 x 4096
-    // 74.2 / 44.5 -> 64.6 / 31.0, 1024 x 1024 x 1376 24.4 / 12.2 -> 22.1 / 12.0, FP8 1024 x 2048 x 2048 29.3 / 13.0 -> 27.7 / 13.1; shorter: FP8 1024 x 1024 x 1376
+    // 74.2 / 44.5 -> 64.6 / 31.0, 1024 x 1024 x 1376 24.4 / 12.2 -> 22.1 / 12.0, FP8 (its own adder) 1024 x 2048 x 2048 29.3 / 13.0 -> 27.7 / 13.1; shorter: FP8 1024 x 1024 x 1376
     // 17.0 / 11.3 -> 17.5 / 11.3, FP16 1024 x 512 x 1376 15.9 / 9.3 -> 16.5 / 9.7
     if (ceil_div(p.M, 128) * ceil_div(p.N, 128) <= cu_count() && p.K * (FP8 ? 1 : 2) >= 2048)
       return launch_one<true, CfgW128, FP8, FA, FB, true, NT, EPI, false>(p, 1, p.K, st);
