@@ -12,7 +12,7 @@ thread_local int g_call_device = kNoCall;
 struct LaunchNote {
   const char* kind;
   int bm, bn, waves_k, nst, epi, splits, waves;
-  bool fp8, a_kc, b_kc, wide;
+  bool fp8, a_kc, b_kc, wide, as_f16;
 };
 constexpr int kMaxNotes = 12;
 thread_local LaunchNote g_notes[kMaxNotes];
@@ -50,8 +50,8 @@ const DeviceInfo& device_info() {
 }
 
 void note_gemm_launch(const char* kind, int bm, int bn, int waves_k, int nst, bool fp8, bool a_kc, bool b_kc, int epi, bool wide,
-                      int splits, int waves) {
-  if (g_note_count < kMaxNotes) g_notes[g_note_count++] = LaunchNote{kind, bm, bn, waves_k, nst, epi, splits, waves, fp8, a_kc, b_kc, wide};
+                      int splits, int waves, bool as_f16) {
+  if (g_note_count < kMaxNotes) g_notes[g_note_count++] = LaunchNote{kind, bm, bn, waves_k, nst, epi, splits, waves, fp8, a_kc, b_kc, wide, as_f16};
 }
 
 const char* last_launch_record() {
@@ -64,9 +64,9 @@ const char* last_launch_record() {
     const int room = (int)sizeof(g_record) - len;
     char waves[16] = "";
     if (n.waves > 0) snprintf(waves, sizeof(waves), ":w%d", n.waves);
-    const int w = snprintf(g_record + len, (size_t)room, "%s%s:%dx%d:wk%d:st%d:%s:%s:%s%s:s%d%s", i ? " + " : "", n.kind, n.bm, n.bn, n.waves_k,
+    const int w = snprintf(g_record + len, (size_t)room, "%s%s:%dx%d:wk%d:st%d:%s:%s:%s%s:s%d%s%s", i ? " + " : "", n.kind, n.bm, n.bn, n.waves_k,
                            n.nst, n.fp8 ? "fp8" : "f16", n.a_kc ? (n.b_kc ? "NT" : "NN") : (n.b_kc ? "TT" : "TN"),
-                           (n.epi >= 0 && n.epi < 14) ? epi_name[n.epi] : "?", n.wide ? ":f32" : "", n.splits, waves);
+                           (n.epi >= 0 && n.epi < 14) ? epi_name[n.epi] : "?", n.wide ? ":f32" : "", n.splits, waves, n.as_f16 ? ":as16" : "");
     if (w < 0 || w >= room) break;
     len += w;
   }

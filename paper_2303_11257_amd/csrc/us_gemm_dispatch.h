@@ -207,7 +207,7 @@ hipError_t launch_one(const GemmProblem& p, int splits, long k_per_split, hipStr
   if constexpr (DIRECT) kern = gemm_direct_kernel<Cfg, FP8, FA, FB, A_KC, B_KC, EPI, WIDE>;
   else kern = gemm_staged_kernel<Cfg, FP8, FA, FB, A_KC, B_KC, EPI, WIDE>;
   note_gemm_launch(DIRECT ? "direct" : "staged", Cfg::BM, Cfg::BN, Cfg::WAVES_K, Cfg::NST, FP8, A_KC, B_KC, EPI, WIDE, splits,
-                   std::is_same<Cfg, CfgQ256>::value ? Cfg::WAVES : 0);
+                   std::is_same<Cfg, CfgQ256>::value ? Cfg::WAVES : 0, (FA & kAsF16) != 0);
   static FuncConfig cfg;           // raising the dynamic-LDS limit: once per function and device
   if (hipError_t e = cfg.ensure((const void*)kern, LDS); e != hipSuccess) return e;
   const GemmArgs g = make_args(p, k_per_split, Cfg::BM, Cfg::BN);
@@ -221,7 +221,7 @@ template <class Cfg, bool FP8, int FA, int FB, bool A_KC, bool B_KC, int EPI, bo
 hipError_t launch_small(const GemmProblem& p, hipStream_t st) {
   constexpr int LDS = SmallTile<Cfg, FP8, A_KC, B_KC>::LDS_BYTES;
   auto kern = gemm_small_kernel<Cfg, FP8, FA, FB, A_KC, B_KC, EPI, WIDE>;
-  note_gemm_launch("direct", Cfg::BM, Cfg::BN, Cfg::WAVES, Cfg::NST, FP8, A_KC, B_KC, EPI, WIDE, 1);
+  note_gemm_launch("direct", Cfg::BM, Cfg::BN, Cfg::WAVES, Cfg::NST, FP8, A_KC, B_KC, EPI, WIDE, 1, 0, (FA & kAsF16) != 0);
   static FuncConfig cfg;
   if (hipError_t e = cfg.ensure((const void*)kern, LDS); e != hipSuccess) return e;
   const GemmArgs g = make_args(p, p.K, Cfg::BM, Cfg::BN);

@@ -317,7 +317,7 @@ template <class Cfg, bool FP8, int F>
 hipError_t launch_small_slices(const GemmProblem& p, int slices, float* partial, hipStream_t st) {
   constexpr int LDS = SmallTile<Cfg, FP8, true, false>::LDS_BYTES;
   auto kern = gemm_small_kernel<Cfg, FP8, F, F, true, false, EPI_PARTIAL, true>;
-  note_gemm_launch("direct", Cfg::BM, Cfg::BN, Cfg::WAVES, Cfg::NST, FP8, true, false, EPI_PARTIAL, true, slices);
+  note_gemm_launch("direct", Cfg::BM, Cfg::BN, Cfg::WAVES, Cfg::NST, FP8, true, false, EPI_PARTIAL, true, slices, 0, (F & kAsF16) != 0);
   static FuncConfig cfg;
   if (hipError_t e = cfg.ensure((const void*)kern, LDS); e != hipSuccess) return e;
   GemmArgs g = make_args(p, slice_length(p.K, slices), Cfg::BM, Cfg::BN);

@@ -418,3 +418,25 @@ def test_codes_of_few_tokens_go_by_exact_sums(T, d, f):
     want = dZ.clamp(-57344, 57344).to(torch.float32).to(torch.float8_e5m2).view(torch.uint8)
     moved = (out["dZ"][:T] != want) & at
     assert int(moved.sum()) <= 2e-5 * int(at.sum()) + 3, (int(moved.sum()), int(at.sum()))
+
+
+@pytest.mark.parametrize("T", [1024, 1025])
+def test_the_launch_record_tells_how_codes_are_added(T):
+    """The sums of Z and dH go by FP16 instructions up to 1024 tokens and by the FP8 ones beyond; the other products by the FP8 ones."""
+    b = Block(T, 64, 96, True, False, us.GATE_SILU)
+    for run in (b.forward, b.backward):
+        run()
+        first, *others = us.last_launch().split(" + ")
+        assert ":fp8:" in first and first.endswith(":as16") == (T <= 1024), first
+        assert others and not any(":as16" in n for n in others), others
+
+
+@pytest.mark.parametrize("T,d,f,up,down", [(9, 2064, 5648, False, True), (32, 4112, 5136, True, True), (33, 2048, 5632, False, True), (64, 1040, 4112, False, True),
+                                           (65, 1040, 4112, False, False), (17, 512, 1376, False, False)])
+def test_a_few_rows_of_codes_in_slices(T, d, f, up, down):
+    """... the same rule in FP8, whose weights have half of the bytes."""
+    b = Block(T, d, f, True, False, us.GATE_SILU, seed=T)
+    b.forward()
+    launches = us.last_launch().split(" + ")
+    assert ["partial" in n for n in launches] == [up, down], launches
+    assert [n.endswith(":as16") for n in launches] == [True, False], launches
