@@ -440,3 +440,24 @@ def test_a_few_rows_of_codes_in_slices(T, d, f, up, down):
     launches = us.last_launch().split(" + ")
     assert ["partial" in n for n in launches] == [up, down], launches
     assert [n.endswith(":as16") for n in launches] == [True, False], launches
+
+
+@pytest.mark.parametrize("keep8", [False, True])
+@pytest.mark.parametrize("T,d,f,forward,dz", [
+    (1100, 2048, 1600, "128x128:wk2", "128x128:wk2"),            # two wave groups in both directions
+    (1027, 2064, 1616, "128x128:wk2", "128x128:wk2"),            # ... tokens, reduction and widths that end inside a tile and a block of 32
+    (1100, 256, 416, "64x64", "32x64"),                          # few tiles
+    (1100, 272, 800, "128x128:wk1", "64x64"),
+    (1040, 144, 208, "32x64", "32x64"),
+])
+def test_tiles_of_the_fp8_adder(T, d, f, forward, dz, keep8):
+    """FP8 with more than 1024 tokens: every tile of few rows of tiles, whose sums are the matrix core's FP8 sums."""
+    b = Block(T, d, f, True, keep8, us.GATE_GELU, seed=T + f)
+    first = b.forward().outputs()
+    taken = us.last_launch().split(" + ")[0]
+    assert forward in taken and ":as16" not in taken, taken
+    check_forward(b, first)
+    out = b.backward().outputs()
+    taken = us.last_launch().split(" + ")[0]
+    assert dz in taken and ":as16" not in taken, taken
+    check_backward(b, out)
