@@ -437,7 +437,10 @@ us_status us_sum_bwd(const void* G, void* dX, long rows, long n, float beta, voi
  *   X [T,d], Wgu [d,2f] (the gate's columns first), Wd [f,d]; T is free (one token upwards, no multiple of anything), d and f are
  *   multiples of 16 from 16 to US_FFN_GATED_MAX.
  *   mode: US_FFN_FP8: operands are E4M3 codes (else FP16) and H receives E4M3 codes (else FP16).  Z's and dH's sums are FP32 sums of exact products for
- *   up to 1024 tokens, the matrix core's FP8 sums (1.3e-5 rms of a unit off) for more.
+ *   up to 1024 tokens, the matrix core's FP8 sums (1.3e-5 rms of a unit off) for more; Y, dX, dWgu and dWd are the latter as us_linear_*'s results are
+ *   (but Y of the few rows whose weights are streamed).  A code of dZ or H next to a border may come out as its neighbour, and so may relu' of a Zg next
+ *   to zero.  That moves single elements of dWgu, the fewer tokens the further: measured with silu and gelu by up to 8 T^-1/2 of the RMS beyond 1024 tokens (a quarter there),
+ *   by 0.1 from 512 to 1024 and 0.2 at 64; the 2-norm of dX and dWgu by 2e-3 beyond and 9e-4 below, of Y and dWd by 1.4e-3 and 4e-4.
  *   H is made from the FP32 sums and rounded once.  Z is what the backward pass needs: FP16, or with US_FFN_KEEP8 8-bit blocks (us_keep8_store's
  *   format, also made from the FP32 sums, the blocks of Zg and of Zu starting at their first columns): codes Z [T,2f] and scales Zs
  *   [T, 2 us_keep8_blocks(f)].  Without US_FFN_KEEP8 Zs is not used and Z may be NULL: nothing is kept (serving).

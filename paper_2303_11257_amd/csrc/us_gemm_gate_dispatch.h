@@ -12,9 +12,13 @@ namespace us {
 using CfgG256 = GemmCfg<256, 256, 4, 2, 128, 2, 1>;
 
 // FP8 products of at most so many tokens go to the matrix core as FP16.  H and dZ are rounded to codes an eighth and a quarter wide: where the FP8 adder moves a
-// code of dZ across a border, a column of dWgu = T^-1/2 X^T dZ moves by step * X * T^-1/2, which few tokens do not average out (14 to 409 tokens of d = 1072 to
-// 2816: single elements off by up to half of the RMS, as FP16 by 0.01; from 1216 on by 0.2 and less).  It costs, us, FP8 -> FP16: forward and backward 14 x 1072 x 2848
+// code of dZ across a border, a column of dWgu = T^-1/2 X^T dZ moves by step * X * T^-1/2, which few tokens do not average out.  The limit is where that is a
+// quarter of the RMS for a step of 2 (codes from 8 to 16; larger ones are a few per tensor) and an X of 4: 8 T^-1/2 = 1/4 at 1024 tokens.  Largest deviation of an
+// element of dWgu from 64 bits, of the RMS, silu and gelu, d = 512 to 2048, FP8 adder / as FP16: 256 tokens 0.47 / 0.13, 512 0.36 / 0.09, 1024 0.25 / 0.10, 1216 0.22 / 0.11,
+// 1536 0.19 / 0.10, 2048 0.17 / 0.08, 4096 0.14 / 0.06; 2-norm 2.0e-3 to 2.6e-3 / 4e-4 to 7e-4 throughout.
+// It costs, us, FP8 -> FP16: forward and backward 14 x 1072 x 2848
 // 45.9 -> 46.1, 409 x 1920 x 7680 158 -> 171, 1024 x 4096 x 11008 621 -> 685; forward 16 x 2048 x 5632 23.5 -> 23.3, 512 x 4096 x 11008 88 -> 131.
+// (The forward call without Z takes it too: what is kept does not change the answer.)
 constexpr long kAsF16Rows = 1024;
 
 // EPI: of the forward product (NN) or of dH (NT).

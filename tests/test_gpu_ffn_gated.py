@@ -461,3 +461,56 @@ def test_tiles_of_the_fp8_adder(T, d, f, forward, dz, keep8):
     taken = us.last_launch().split(" + ")[0]
     assert dz in taken and ":as16" not in taken, taken
     check_backward(b, out)
+
+
+def nearest_codes(v, bits, least, top):
+    """Values of the nearest FP8 codes (`bits` behind the leading one, exponents from `least`, clipped at `top`), and the step at each."""
+    step = torch.exp2(torch.floor(torch.log2(v.abs().clamp_min(2.0 ** least))) - bits)
+    return ((v / step).round() * step).clamp(-top, top), step
+
+
+@pytest.mark.parametrize("T", [512, 1024, 1025, 1400])
+def test_gradients_end_to_end_on_both_sides_of_1024_tokens(T):
+    """dX, dWgu and dWd against 64 bits from the operands' codes on, no tensor of the GPU's in between.
+
+    What separates them are codes of dZ and H that fall on the other side of a border, each of which moves a value by its step, and Zg next to zero whose
+    relu' comes out for the other sign, which moves dZ by all of its value; next to FP16's rounding of the results and the products' sums (3e-4 of the
+    2-norm together, see above).  A sum that is off by e moves a code with probability |e| / step and a sign with |e| times a unit normal's density at
+    zero.  |e| is on average 4/5 of the sum's rms error (normal), 1.3e-5 for the FP8 adder and 4e-8 for sums of exact products, times the derivative
+    towards Zg, Zu and dH (kept Z's own rounding passes a shift on, on average); for dZ and H themselves five roundings of 2^-25 on average.  The
+    moved energy therefore has the mean sum p E and the variance sum p E^2 over all elements (p: probability, E: the move's square): four standard deviations
+    are allowed.  A product of independent operands keeps the ratio of 2-norms.
+    Single elements: a code from 8 to 16 of dZ (step 2; larger ones are a few per tensor) next to an operand of 4 moves an element of dWgu by
+    8 T^-1/2 of a unit, an eighth of that for dX, whose sum has 2f terms; H's steps are half as large.  Signs: no sum is off by more than 2e-4 of a
+    unit with FP8 operands (parity.py), 2e-6 being 50 times the rms error of exact products' sums; whatever lies closer to zero may move."""
+    d, f = 528, 1040
+    b = Block(T, d, f, True, False, us.GATE_RELU, seed=T)
+    b.forward()
+    assert ":as16" in us.last_launch() or T > 1024
+    out = b.backward().outputs()
+    X, Wgu, Wd, G = operand(b.X), operand(b.Wgu), operand(b.Wd), operand(b.G, True)
+    alpha, beta = (float(np.float32(v)) for v in us.gate_scales(us.GATE_RELU))
+    Z = X @ Wgu / math.sqrt(d)
+    on, near = (Z[:, :f] > 0).double(), (Z[:, :f].abs() <= (2e-6 if T <= 1024 else 2e-4)).double()
+    H, h_step = nearest_codes(alpha * on * Z[:, :f] * Z[:, f:], 3, -6, 448.0)
+    zg, zu = (z.half().double() for z in (Z[:, :f], Z[:, f:]))
+    dH = G @ Wd.t() / math.sqrt(d)
+    dZ, z_step = nearest_codes(torch.cat([beta * on * zu * dH, alpha * on * zg * dH], 1), 2, -14, 57344.0)
+    unit = 0.8 * (4e-8 if T <= 1024 else 1.3e-5)
+    e_z = unit * torch.cat([beta * on * (zu.abs() + dH.abs()), alpha * on * (zg.abs() + dH.abs())], 1) + 5 * 2.0 ** -25 * dZ.abs()
+    e_h = unit * alpha * on * (zg.abs() + zu.abs()) + 5 * 2.0 ** -25 * H.abs()
+    sign = beta * zu * dH
+
+    def most_energy(*moves):
+        mean, var = (sum(float((p * e.square() ** k).sum()) for p, e in moves) for k in (1, 2))
+        return mean + 4 * math.sqrt(var)
+
+    of_z = math.sqrt(most_energy((e_z / z_step, z_step), (unit * (2 * math.pi) ** -0.5, sign)) / float(dZ.square().sum()))
+    of_h = math.sqrt(most_energy((e_h / h_step, h_step)) / float(H.square().sum()))
+    jump = torch.cat([sign.abs() * near, torch.zeros_like(sign)], 1)
+    for name, want, moved, jumps in (("dX", dZ @ Wgu.t() / math.sqrt(2 * f), of_z, jump @ Wgu.abs().t() / math.sqrt(2 * f)),
+                                     ("dWgu", X.t() @ dZ / math.sqrt(T), of_z, X.abs().t() @ jump / math.sqrt(T)), ("dWd", H.t() @ G / math.sqrt(T), of_h, 0.0)):
+        diff, rms = (out[name][:-1].double() - want).abs(), float(want.square().mean().sqrt())
+        off = float(diff.square().mean().sqrt()) / rms
+        assert off <= 3e-4 + moved, (name, off, moved)
+        assert (diff <= 8 / math.sqrt(T) * rms + jumps).all(), (name, float((diff - jumps).max()) / rms)
