@@ -497,7 +497,7 @@ us_status us_keep8_load(const void* codes, const void* scales, void* X, long ld,
  *         variance; v's too);  dw = fp16(beta_w sum g x^), beta_w <= 0: (rows)^-1/2 with rows = batch s heads (wq) or batch s kv_heads (wk);
  *         dx = fp16(rstd (g w - x^ mean(g w x^)))  -> dQKV, laid out as QKV with row pitch ld_d; columns beyond the heads are left as they were
  * wq, wk: FP16 [dh], or NULL for ones.  pos: int32 [batch * s] (any value), or NULL: the place in the sequence.  freq: double [rot / 2],
- * radians per position, finite (may be NULL if rot = 0); an angle is right to 2^-25 of a turn for every position.  dwq, dwk: FP16 [dh]
+ * radians per position, finite (may be NULL if rot = 0); up to 2^40 an angle is right to 2^-25 of a turn at every position.  dwq, dwk: FP16 [dh]
  * or NULL.  dh a multiple of 16 up to US_ROPE_HEAD_MAX; rot a multiple of 16 up to dh; kv_heads divides heads <= 65535; eps >= 0 (0: a
  * head of zeros gives NaN).  The workspace (us_qk_norm_rope_workspace_bytes, 16-byte aligned, undefined on entry and exit) holds partial sums
  * of the weights' gradients, added in a fixed order.  Outputs must not overlap inputs or one another.

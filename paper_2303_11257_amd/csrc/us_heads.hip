@@ -11,7 +11,7 @@
 // A power of two of such lane groups takes a token at a time: the angles depend on the token and the lane only and are made once for all of
 // its heads.
 // Angles: a frequency is held as a 64-bit fraction of a turn per position, position * frequency modulo 1 is then integer arithmetic
-// that drops whole turns exactly, for any 32-bit position; v_sin / v_cos take the rest, in turns.
+// that drops whole turns exactly, for any 32-bit position and frequencies of many turns; v_sin / v_cos take the rest, in turns.
 #include <type_traits>
 
 #include "us_device.h"
@@ -44,6 +44,17 @@ __device__ __forceinline__ float head_sum(float v) {
   return v;
 }
 
+// radians -> turns as a 64-bit fraction of one, whole turns dropped.  1 / 2 pi is the sum of two doubles; the product's rounding and the second part are
+// kept in `rest`.  Everything in units of 2^-32 turns; adding 1.5 * 2^52 rounds to a whole number, which is then the low bits of the sum.  For frequencies up to
+// 2^40 the fraction is right to its last bit, and so an angle at any position to 2^-31 of a turn before its FP32 rounding (2^-26).
+__device__ __forceinline__ uint64_t turn_fraction(double w) {
+  constexpr double kHi = 0x1.45f306dc9c883p+29, kLo = -0x1.6b01ec5417056p-25, kMagic = 0x1.8p52;
+  double t = w * kHi;
+  const double rest = __builtin_fma(w, kLo, __builtin_fma(w, kHi, -t));
+  t = __builtin_fma(__builtin_rint(t * 0x1p-32), -0x1p32, t);      // at most half a turn
+  const double whole = (t + rest) + kMagic, low = __builtin_fma((t - (whole - kMagic)) + rest, 0x1p32, kMagic);
+  return (__builtin_bit_cast(uint64_t, whole) << 32) + (__builtin_bit_cast(uint64_t, low) - __builtin_bit_cast(uint64_t, kMagic));
+}
 // The lane's eight frequencies as 64-bit fractions of a turn, and their angles at a position.
 struct LaneAngles {
   uint32_t hi[8], lo[8];
@@ -55,10 +66,9 @@ struct LaneAngles {
       c[k] = 1.0f;
       s[k] = 0.0f;
       if (rotated) {
-        double t = freq[first + k] * 0.15915494309189533577;      // turns per position
-        t = (t - __builtin_floor(t)) * 4294967296.0;
-        hi[k] = (uint32_t)t;
-        lo[k] = (uint32_t)((t - __builtin_floor(t)) * 4294967296.0);
+        const uint64_t f = turn_fraction(freq[first + k]);
+        hi[k] = (uint32_t)(f >> 32);
+        lo[k] = (uint32_t)f;
       }
     }
   }

@@ -8,6 +8,7 @@ the mean over the head, so 2^-15 of the largest magnitude of the head's gradient
 a chain of at most (tokens / groups * heads + groups) terms, 2^-14 of the sum of magnitudes being far above it for the sizes here.
 """
 import math
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -215,3 +216,27 @@ def test_captured_on_another_stream_and_two_at_once():
             n, cols = batch * h * s * dh, (h + 2 * kv) * dh
             assert all(torch.equal(ef[k][:n], of[k][:n]) for k in "QKV")
             assert torch.equal(eb["dx"][:, :cols], ob["dx"][:, :cols]) and torch.equal(eb["dwq"], ob["dwq"]) and torch.equal(eb["dwk"], ob["dwk"])
+
+
+PI = Fraction("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211706798")
+
+
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_every_frequency_at_every_position(neighbours):
+    """Large, negative, tiny and tiny negative frequencies at the ends of 32-bit positions, against angles from rational arithmetic (102 digits of pi)."""
+    freqs = [37.0, 1e3, 1e6, -5.5e5, 2.0 ** 33 / 3, -2.0 ** 40, 1e-19, -1e-19, -4e-17, 1e-12, 2 * math.pi, -2 * math.pi, math.pi, 0.0, 0.1, 6.0]
+    pos = [2 ** 31 - 1, -2 ** 31, 1234567891, -987654321, -1, 1, 0, 65537]
+    batch, s, h, kv, dh, rot = 1, len(pos), 2, 1, 48, 32
+    ld = (h + 2 * kv) * dh
+    m = make(batch, s, h, kv, dh, rot, ld, seed=11)
+    m["pos"], m["freq"] = torch.tensor(pos, dtype=torch.int32), torch.tensor(freqs, dtype=torch.float64)
+    turns = [[p * Fraction(f) / (2 * PI) % 1 for f in freqs] for p in pos]
+    angle = torch.tensor([[float(t if t <= Fraction(1, 2) else t - 1) * 2 * math.pi for t in row] for row in turns], dtype=torch.float64)
+    ref = reference(m, batch, s, h, kv, dh, 0, neighbours, 1e-6, False)
+    i = torch.arange(rot // 2)
+    a, b = (2 * i, 2 * i + 1) if neighbours else (i, i + rot // 2)
+    for k in "QK":
+        y = ref[k].clone()
+        ref[k][..., a] = y[..., a] * angle.cos() - y[..., b] * angle.sin()
+        ref[k][..., b] = y[..., b] * angle.cos() + y[..., a] * angle.sin()
+    check(forward(to_gpu(m), batch, s, h, kv, dh, rot, ld, neighbours, 1e-6), ref, m, batch, s, h, kv, dh, rot, ld)
