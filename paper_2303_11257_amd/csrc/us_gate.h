@@ -19,14 +19,16 @@ struct GateTerms {
 };
 // gate: 0 silu, 1 gelu, 2 relu, 3 sigmoid (us_gate).  One exponential and one reciprocal for silu and sigmoid: p = 1 / (1 + 2^(-z log2 e)) keeps
 // its relative accuracy on both sides; 1 - p loses it only where it is small next to the terms it is added to.  From z = -88 on the exponential
-// is infinite and p zero, as f and f' are in every result type.  (sigmoid' needs p e, so its exponent stops at 126.)  A NaN gives NaN.
+// is infinite and p zero, as f and f' are in every result type.  (sigmoid' needs p e, so its exponent stops at 126.)  A NaN gives NaN in both, and so do infinite
+// z of silu and gelu where a limit would have to be taken (0 times infinity).
 template <int GATE>
 __device__ __forceinline__ GateTerms gate_terms(float z) {
   if constexpr (GATE == 1) {
     const GaussTerms g = gauss_terms(z);
     return {z * g.Phi, __builtin_fmaf(z, g.pdf, g.Phi)};
   } else if constexpr (GATE == 2) {
-    return {z <= 0.0f ? 0.0f : z, z > 0.0f ? 1.0f : 0.0f};
+    const float f = z <= 0.0f ? 0.0f : z;
+    return {f, f > 0.0f ? 1.0f : f};
   } else {
     float x = -1.4426950408889634f * z;
     if constexpr (GATE == 3) x = x > 126.0f ? 126.0f : x;

@@ -514,3 +514,21 @@ def test_gradients_end_to_end_on_both_sides_of_1024_tokens(T):
         off = float(diff.square().mean().sqrt()) / rms
         assert off <= 3e-4 + moved, (name, off, moved)
         assert (diff <= 8 / math.sqrt(T) * rms + jumps).all(), (name, float((diff - jumps).max()) / rms)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("gate", range(4))
+@pytest.mark.parametrize("T,f", [(5, 80), (700, 2064)])
+def test_a_nan_of_the_gate_is_one_in_its_column(T, f, gate, fp8):
+    """A NaN weight of the gate's half makes its columns of Z, H and dZ NaN, whatever the gate, and no other column of Z and dZ."""
+    for keep8 in (False, True):
+        b = Block(T, 64, f, fp8, keep8, gate, seed=2)
+        b.g["Wgu"][3, 7] = 0x7f if fp8 else float("nan")
+        out = b.forward().backward().outputs()
+        zg, zu = kept(b, out)
+        H, dZ = operand(out["H"][:T]), operand(out["dZ"][:T], True)
+        hit = torch.zeros(2 * f, dtype=torch.bool)
+        hit[7] = hit[f + 7] = True
+        assert torch.isnan(zg[:, 7]).all() and not torch.isnan(zg[:, ~hit[:f]]).any() and not torch.isnan(zu).any()
+        assert torch.isnan(H[:, 7]).all() and not torch.isnan(H[:, ~hit[:f]]).any()
+        assert torch.isnan(dZ[:, hit]).all() and not torch.isnan(dZ[:, ~hit]).any(), [int(torch.isnan(dZ[:, c]).sum()) for c in (7, f + 7)]
