@@ -478,7 +478,8 @@ size_t us_ffn_gated_workspace_bytes(long T, long d, long f, int mode);
  *          64 for a block with a NaN
  *   load:  the values that the codes stand for, which FP16 holds exactly; elements of X beyond column n of a row are left as they were
  * n a multiple of 16, ld >= n a multiple of 8; rows is free; all pointers 16-byte aligned.  The error of a value is at most half a
- * step, below 2^-7 of the block's largest magnitude.  us_keep8_blocks(n) = ceil(n / 32).
+ * step, and half a step at most 1/127.5 of the block's largest magnitude where that is at least 127.5 * 2^-24 (below, values are exact); finite values
+ * beyond 127.5 * 2^9 = 65280 are held as 65024, up to 480 off.  us_keep8_blocks(n) = ceil(n / 32).
  */
 long us_keep8_blocks(long n);
 us_status us_keep8_store(const void* X, long ld, void* codes, void* scales, long rows, long n, void* stream);

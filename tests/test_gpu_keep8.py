@@ -76,3 +76,21 @@ def test_captured_and_replayed_on_another_stream():
         graph.replay()
         ec, es = R.keep8(v.astype(np.float64))
         assert np.array_equal(to_np(back).astype(np.float64), R.keep8_values(ec, es), equal_nan=True)
+
+
+def test_the_error_of_a_value_is_within_the_stated_bound():
+    """Every finite FP16 value as the largest of its block, next to values at the codes' borders (a half, one and a half ... steps of either candidate)."""
+    bits = np.arange(65536, dtype=np.uint16).view(np.float16)
+    big = np.abs(bits[np.isfinite(bits)]).astype(np.float64)
+    x = np.concatenate([big[:, None] * np.array([1.0] + [k / 127.5 * h for k in (0.5, 1.0, 1.5, 63.5, 64.5, 126.5) for h in (0.5, 1.0, -1.0)])[None], np.zeros((len(big), 13))], 1)
+    x = np.where(np.abs(x) <= big[:, None], x, big[:, None]).astype(np.float16)
+    codes, scales, c, s = store(to_dev(x), 32, len(x), 32)
+    back = torch.empty((len(x), 32), dtype=torch.float16, device=DEV)
+    us.keep8_load(ptr(codes), ptr(scales), ptr(back), 32, len(x), 32, stream())
+    x = x.astype(np.float64)
+    off, most = np.abs(to_np(back).astype(np.float64) - x), np.abs(x).max(1)
+    clipped = np.abs(x) > 127.5 * 512
+    half = np.exp2(s.astype(np.float64) - 128.0)
+    assert (off <= half)[~clipped].all() and (off[clipped] <= 480).all() and clipped.any()
+    small = most < 127.5 * 2.0 ** -24
+    assert (half[:, 0] <= most / 127.5)[~small].all() and (half[:, 0] == most / 127.5).any() and (off[small] == 0).all()
