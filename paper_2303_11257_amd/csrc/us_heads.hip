@@ -355,8 +355,9 @@ __global__ void __launch_bounds__(kThreads) heads_dw_kernel(const float* __restr
 // Workgroups of the backward kernel: one per wave that its registers leave a SIMD, so that all run at once and each makes its frequencies and its row of sums once
 // (us, four per CU -> this: 65536 tokens of 12 + 2 x 12 heads of 64 264 -> 216, 16384 of 1 + 2 x 1 of 64 17.0 -> 13.3, 16384 of 32 + 2 x 8 of 128
 // 185 -> 178), or one per token.
-long bwd_groups(long tokens, long dh) {
-  const long most = (dh <= 64 ? 3 : 2) * (long)device_info().cus;
+constexpr long kMostCus = 256;     // of a gfx950 device; partitions have fewer
+long bwd_groups(long tokens, long dh, long cus) {
+  const long most = (dh <= 64 ? 3 : 2) * (cus < kMostCus ? cus : kMostCus);
   return tokens < most ? tokens : most;
 }
 // Lane groups (2^lg) on a token: as many as it has heads, up to `most`.
@@ -392,7 +393,7 @@ HeadsArgs heads_args(const HeadsCall& c) {
 }  // namespace
 
 // (the most rows any device's grid makes: the size does not depend on which device asks)
-size_t heads_workspace_bytes(long tokens, long dh) { return (size_t)bwd_groups(tokens, dh) * 2 * (size_t)dh * sizeof(float); }
+size_t heads_workspace_bytes(long tokens, long dh) { return (size_t)bwd_groups(tokens, dh, kMostCus) * 2 * (size_t)dh * sizeof(float); }
 
 constexpr long kFwdPerCu = 16;     // workgroups per CU: three rounds of what its registers allow even out better than one
 // From so many tokens per CU on a wave has one of its own and makes its angles once, as in the backward kernel.  us, four waves on a token -> one: 65536 tokens of
@@ -411,7 +412,7 @@ hipError_t launch_heads_fwd(const HeadsCall& c, void* Q, void* K, void* V, hipSt
 
 hipError_t launch_heads_bwd(const HeadsCall& c, const void* dQ, const void* dK, const void* dV, void* dQKV, long ld_dx, void* dwq, void* dwk,
                             float beta_wq, float beta_wk, void* workspace, hipStream_t st) {
-  const long rows = bwd_groups(c.batch * c.s, c.dh);
+  const long rows = bwd_groups(c.batch * c.s, c.dh, device_info().cus);
   float* partial = (float*)workspace;
   const float rep_scale = (float)(1.0 / __builtin_sqrt((double)(c.heads / c.kv_heads)));
   const hipError_t e = with_shape(c.dh, c.pairs, [&](auto g, auto halves) {
