@@ -453,7 +453,8 @@ us_status us_sum_bwd(const void* G, void* dX, long rows, long n, float beta, voi
  *   (skipped).  dH is never stored or rounded.  Zg and Zu are the kept values.  H: without US_FFN_KEEP8 the forward call's; with it,
  *   scratch that this call fills again from the kept values with the factor alpha (the forward call's H need not live until then).
  *   With T = 0 the weights' gradients are zeros.
- * Workspace (16-byte aligned, contents undefined on entry and exit): us_ffn_gated_workspace_bytes serves both; the forward call can do
+ *   A Zg beyond FP16's range is kept as an infinity (in 8-bit blocks clipped), whose dZ is NaN with silu and gelu.
+ * Workspace (16-byte aligned, contents undefined on entry and exit): us_ffn_gated_workspace_bytes, asked with the device current that runs the calls, serves both; the forward call can do
  * without (NULL; up to 64 tokens it is then slower and adds in another order), the backward call needs it where a weight's gradient is cut into
  * slices, as us_linear_bwd does.  Calls that may overlap on a GPU need a workspace each.
  * Outputs must not overlap inputs or one another.  A gate outside the list is US_ERR_DTYPE, an unknown mode bit US_ERR_VALUE.
@@ -501,7 +502,13 @@ us_status us_keep8_load(const void* codes, const void* scales, void* X, long ld,
  * radians per position, finite (may be NULL if rot = 0); up to 2^40 an angle is right to 2^-25 of a turn at every position.  dwq, dwk: FP16 [dh]
  * or NULL.  dh a multiple of 16 up to US_ROPE_HEAD_MAX; rot a multiple of 16 up to dh; kv_heads divides heads <= 65535; eps >= 0 (0: a
  * head of zeros gives NaN).  The workspace (us_qk_norm_rope_workspace_bytes, 16-byte aligned, undefined on entry and exit) holds partial sums
- * of the weights' gradients, added in a fixed order.  Outputs must not overlap inputs or one another.
+ * of the weights' gradients, added in a fixed order; it is needed whether or not they are asked for.  Without tokens nothing is written.  Outputs must
+ * not overlap inputs or one another.
+ *
+ * us_attention_* then wants s a multiple of 16, the same s for queries and keys, and takes no mask: one token of generation, an odd s and a causal
+ * layer go on to the caller's own attention.  The projection's gradients: with shared heads dQKV's key and value columns carry (heads / kv_heads)^-1/2,
+ * which a weight's gradient may (it is a cut-edge, column by column) and the projection's input gradient, which adds all columns, may not (Sec. 5.2 step 2):
+ * for a multiple of the loss's gradient give dQ the same factor first (us_weighted_add(dQ, dQ, dQ, n, US_F16, c, 0)).
  */
 typedef enum { US_ROPE_HALVES = 0, US_ROPE_NEIGHBOURS = 1 } us_rope_pairs;
 #define US_ROPE_HEAD_MAX 256

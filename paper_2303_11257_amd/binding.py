@@ -396,7 +396,7 @@ def ffn_gated_fwd(X, Wgu, Wd, Z, Zs, H, Y, T, d, f, gate=GATE_SILU, mode=0, work
 def ffn_gated_bwd(X, Wgu, Wd, Z, Zs, H, G, dZ, dX, dWgu, dWd, T, d, f, gate=GATE_SILU, mode=0, workspace=None, workspace_bytes=0, stream=None,
                   alpha=0.0, beta_gate=0.0, beta_up=0.0):
     """With FFN_KEEP8 H is scratch that the call fills from the kept values.  beta_gate = beta_up for gradients of X and Wgu that are a
-    multiple of the loss's (include/us.h)."""
+    multiple of the loss's, as a model's training needs them (include/us.h); the defaults give either half unit variance on its own."""
     status = (_lib or lib()).us_ffn_gated_bwd(X, Wgu, Wd, Z, Zs, H, G, dZ, dX, dWgu, dWd, T, d, f, gate, int(mode), alpha, beta_gate, beta_up,
                                               workspace, workspace_bytes, stream)
     if status:

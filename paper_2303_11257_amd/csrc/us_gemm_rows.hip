@@ -6,13 +6,12 @@
 // instructions, whose operands would have to be transposed on the way.  (FP16: v_fma_mix takes the halves as they are; FP8: two values per
 // conversion.  Per 16 bytes of weights of a lane 8 T, FP8 8 + 16 T instructions.)
 // A workgroup takes 256 bytes of columns and a slice of the rows; its 4 waves take 16 rows at a time, 4 for each of a wave's
-// four groups of 16 lanes, two such batches in flight.  Slices are as many as give every CU two workgroups; their FP32 sums are
-// added in order by a second kernel, which also makes the gate (nothing else knows a whole sum).
+// four groups of 16 lanes, two such batches in flight.  Slices are as many as give every CU four workgroups for one and two rows, three for three and
+// four, two for more; their FP32 sums are added in order by a second kernel, which also makes the gate (nothing else knows a whole sum).
 // One FP8 token, 4096 x 11008: first projection 18.8 us = 4.8 TB/s, second 11.2 us = 4.0, the two sums 4.6 and 3.8, which is little more than a launch; a
 // large copy reaches 5.1 TB/s.
 // (The second projection's workgroups making H from the slices themselves, each for its rows while their first weights are on the way, save
-// that kernel and cost as much: one FP8 token, 4096 x 11008, 39.4 us with it, 40.0 without.  Three batches in flight instead of two: 19.0 us
-// of the first projection against 20.7.)
+// that kernel and cost as much: one FP8 token, 4096 x 11008, 39.4 us with it, 40.0 without.)
 #include <type_traits>
 
 #include "us_gemm_gate_dispatch.h"
