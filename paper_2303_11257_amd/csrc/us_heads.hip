@@ -3,10 +3,10 @@
 //             repeated for the query heads that share them
 //   backward  g = R^-1(dy) (K, V: the sharing heads' gradients added in FP32, times repeats^-1/2);  dw = beta sum g x^;
 //             dx = rstd (g w - x^ mean(g w x^))
-// Bound: HBM; every value is read and written once: 16384 tokens of 32 query and 2 x 8 shared heads of 128, forward 604 MB in 118 us = 5.1 TB/s (a large copy: 5.1),
-// backward 805 MB in 178 us = 4.5, bound by two waves per SIMD (in heads above 64 the weights' sums and the angles stay in registers; held to three or
-// four, the compiler spills: 208 and 323 us).  Heads of 64 and 96 have half of the bytes per angle: forward 4.5 and 3.0 TB/s,
-// backward 4.2 (three waves) and 3.1.  A lane holds 16 values of a head as two chunks of 8 that are each other's partners in the
+// Bound: HBM; every value is read and written once: 16384 tokens of 32 query and 2 x 8 shared heads of 128, forward 604 MB in 129 us = 4.7 TB/s (a large copy: 5.1),
+// backward 805 MB in 177 us = 4.6, bound by two waves per SIMD (in heads above 64 the weights' sums and the angles stay in registers; held to three or
+// four, the compiler spills: 208 and 323 us).  Heads of 64, 80 and 96 have fewer bytes per angle: forward 4.4, 2.7 and 3.0 TB/s,
+// backward 4.2 (three waves), 2.6 and 3.0.  A lane holds 16 values of a head as two chunks of 8 that are each other's partners in the
 // rotation (or hold whole pairs), dh / 16 neighbouring lanes a head, so the norm's sum stays inside 16 lanes and no value changes lanes.
 // A power of two of such lane groups takes a token at a time: the angles depend on the token and the lane only and are made once for all of
 // its heads.

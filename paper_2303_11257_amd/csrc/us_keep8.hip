@@ -1,5 +1,5 @@
 // 8-bit checkpoints of FP16 activations: rows in blocks of 32 values that share a power of two (us_gate.h says how a block is held).
-// Bound: HBM, 2 + 1 + 1/32 bytes a value in either direction; 16384 x 8192 of rows 12288 apart: store 77 us = 5.3 TB/s, load 73 us = 5.6 (a large copy: 5.1);
+// Bound: HBM, 2 + 1 + 1/32 bytes a value in either direction; 16384 x 8192 of rows 12288 apart: store 76 us = 5.3 TB/s, load 72 us = 5.6 (a large copy: 5.1);
 // short rows, 1048576 x 16: 13.8 and 12.5 us, 3.7 and 4.1 TB/s.  A call of a few rows is its launch, 2.7 us on the device.  A thread holds 8 consecutive values, four neighbouring lanes a block, so the
 // block's largest magnitude takes two exchanges inside a quad of lanes.
 #include <type_traits>
