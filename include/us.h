@@ -79,7 +79,7 @@ typedef struct {
 const char* us_status_string(us_status s);
 
 /* Diagnostics (host only).  Text describing the matmul kernels that the calling host thread's most recent matmul call
- * (us_linear_*, us_ffn_*, us_matmul_batched, us_attention_*) enqueued, one entry per kernel joined by " + ":
+ * (us_linear_*, us_ffn_*, us_matmul_batched, us_attention_fwd, us_attention_bwd) enqueued, one entry per kernel joined by " + ":
  *   kind:BMxBN:wk<wave groups>:st<stages>:<fp8|f16>:<NN|NT|TN>:<epilogue>[:f32]:s<K slices>[:w<waves>][:as16]
  * (waves of a workgroup: only where the rest does not tell two kernels apart; as16: FP8 codes that go to the matrix core as FP16)
  * kind is "direct" (direct-to-LDS loads), "stream" (a few rows by a weight matrix read once, in slices), "staged" (register-staged fallback for row pitches of 16 MB and more), "pair" (two
@@ -520,6 +520,85 @@ us_status us_qk_norm_rope_bwd(const void* QKV, long ld, const void* wq, const vo
                               long kv_heads, long dh, long rot, us_rope_pairs pairs, float eps, float beta_wq, float beta_wk, void* workspace,
                               size_t workspace_bytes, void* stream);
 size_t us_qk_norm_rope_workspace_bytes(long batch, long s, long heads, long kv_heads, long dh);
+
+/*
+ * Heads of a tensor in memory: head h of token t of batch item b starts `batch` b + `head` h + `row` t elements behind the tensor's pointer, its values one
+ * after the other.  All three multiples of 8, batch and head not negative, row from the head's size to US_LAYOUT_ROW_MAX.  Where a layout may be NULL that
+ * selects [batch * heads, s, dh], as us_qk_norm_rope_fwd leaves its heads; a projection's tokens, one head beside the other, are {s * ld, dh, ld}.
+ */
+typedef struct {
+  long batch, head, row;
+} us_heads_layout;
+#define US_LAYOUT_ROW_MAX (1 << 22)
+
+/*
+ * Attention over another sequence's keys (a decoder's over its encoder's states): sq queries over the first n_b of sk keys of batch item b,
+ * n_b = klen[b] (device, int32 [batch], clamped to 0 .. sk) or sk (klen NULL).  Nothing is a multiple of anything but the head's size; scores are not stored.
+ *   fwd:  p = softmax over j < n_b of (dh^-1/2 q k_j);  O = fp16(alpha sum_j p_j v_j);  lse = ln sum_j exp(dh^-1/2 q k_j) (FP32 [batch * heads, sq], may be NULL;
+ *         the backward call reads it)                    alpha <= 0 selects n_b^1/2: what the factors of us_attention_fwd, s and s^-1/2, make together
+ *   bwd:  g = alpha dO;  dp_j = g v_j;  ds_j = p_j (dp_j - sum p dp)
+ *         dQ = fp16(beta_q dh^-1/2 sum_j ds_j k_j)                  beta_q <= 0 selects 1
+ *         dK_j = fp16(beta_kv dh^-1/2 sum ds_j q),  dV_j = fp16(beta_kv sum p_j g), sums over the queries of the heads that share the key head
+ *                                                                   beta_kv <= 0 selects (sk / sq * kv_heads / heads)^1/2: unit variance
+ *         Each of the three is a multiple of the loss's gradient: beta_kv = beta_q = 1 for the gradients themselves.
+ *   Without keys (n_b = 0) O, dQ are 0 and lse is -inf; a single key's dQ and dK are 0.  dK and dV of keys from n_b on are 0; K and V there are not read into
+ *   any result, whatever they hold.  Without queries dK and dV are zeros.
+ * Q, O, dO, dQ: FP16, `heads` heads of sq tokens; K, V, dK, dV: FP16, kv_heads heads of sk tokens; kv_heads divides heads (query head i takes key head
+ * i / (heads / kv_heads)); dh a multiple of 16 up to US_ROPE_HEAD_MAX.  lq: layout of Q and dQ, lkv: of K, V, dK and dV, lo: of O and dO (host pointers, each may
+ * be NULL).  Keys and values that several batch items share have a batch stride of 0 in the forward call; heads and rows of the tensors that a call
+ * writes must not overlap (US_ERR_SHAPE).
+ * Scores, statistics and all sums are FP32; p, alpha p and ds are rounded to FP16 for their second product, as us_attention_* rounds P and dA (values beyond
+ * FP16's range become infinities).  O is read in the backward pass for sum p dp = dO O / alpha.
+ * Workspace (16-byte aligned, contents undefined on entry and exit): us_attention_cross_workspace_bytes, asked with the device current that runs the calls,
+ * serves both.  The forward call can do without (NULL: few queries over many keys are then slower, and are added in another order); the backward call needs it.
+ * Calls that may overlap on a GPU need a workspace each.  Outputs must not overlap inputs or one another.
+ */
+us_status us_attention_cross_fwd(const void* Q, const void* K, const void* V, const int* klen, void* O, float* lse, long batch, long heads, long kv_heads, long sq,
+                                 long sk, long dh, float alpha, const us_heads_layout* lq, const us_heads_layout* lkv, const us_heads_layout* lo, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+us_status us_attention_cross_bwd(const void* Q, const void* K, const void* V, const int* klen, const void* O, const float* lse, const void* dO, void* dQ, void* dK,
+                                 void* dV, long batch, long heads, long kv_heads, long sq, long sk, long dh, float alpha, float beta_q, float beta_kv,
+                                 const us_heads_layout* lq, const us_heads_layout* lkv, const us_heads_layout* lo, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+size_t us_attention_cross_workspace_bytes(long batch, long heads, long kv_heads, long sq, long sk, long dh);
+
+/*
+ * A paged key-value cache for generation.  k_cache and v_cache: pools [pages, kv_heads, page, dh] of FP16 or E4M3 values (cache_dt; unit variance needs no scale),
+ * page = a power of two from 16 to US_CACHE_PAGE_MAX positions.  table: device, int32 [batch, table_ld]; position i of sequence b lies in slot i % page of page
+ * table[b, i / page].  An entry outside 0 .. pages - 1 is a page that there is not: nothing is written there, and no attention goes there.  len: device,
+ * int32 [batch], the positions of each sequence, those of the current call's tokens among them.
+ *
+ * us_cache_store: the last s positions of each sequence, or the last count[b] <= s of them (device, int32 [batch]; NULL: s), from the first s or count[b] tokens of K and V
+ *   (FP16, layout `l`, NULL: [batch * kv_heads, s, dh]; the heads that us_qk_norm_rope_fwd repeats are skipped by a larger head stride).  FP16 is copied, E4M3 is the
+ *   saturating cast of us_cast_fp8 with scale 1.  Positions before the first or behind the table are left out.
+ *
+ * us_attention_paged: one new token per sequence over its n_b = len[b] positions (clamped to 0 .. max_len and to the table):
+ *     p = softmax over i < n_b of (dh^-1/2 q k_i);  O = fp16(alpha sum p_i v_i)           alpha <= 0 selects n_b^1/2, as us_attention_cross_fwd's
+ *     weights[page, key head, slot] += sum of p_i over the query heads that share the key head      (FP32, laid out as the pools' slots; may be NULL)
+ *   Q: FP16 [batch, heads * dh], rows ldq elements apart (a multiple of 8); O likewise, ldo.  max_len: the host's bound on the lengths: the work is shared out for
+ *   it, and longer sequences are cut off there.  Without positions O is 0.  A slot that several positions of the call share must not have weights: their additions race.
+ *   FP32 sums; p is rounded to FP16 for the product with V.  Workspace (16-byte aligned, undefined on entry and exit): us_attention_paged_workspace_bytes, asked with
+ *   the device current that runs the call.
+ *
+ * us_cache_evict: of each sequence that is longer than `keep`, for every key head, the last `recent` positions and the keep - recent others with the largest weights
+ *   (the lower position among equals, a NaN above all numbers) move to positions 0 .. keep - 1, in their order, with their weights; shorter ones stay whole.
+ *   table_to == table: in place; the slots behind are left as they were, and a page must belong to one sequence only.  Another table_to (int32
+ *   [batch, table_to_ld], pages of the same pools that hold none of the sequences): the kept rows are copied there.
+ *   new_len[b] = min(len[b], keep) (int32 [batch], may be len itself, or NULL), kept: int32 [batch, kv_heads, keep], the positions that were kept, -1 behind a shorter
+ *   sequence's.  0 <= recent <= keep.  max_len as above.
+ *
+ * dh a multiple of 16 up to US_ROPE_HEAD_MAX; batch and heads up to 65535.  All pools and rows 16-byte aligned.  Results do not depend on scheduling.
+ */
+#define US_CACHE_PAGE_MAX 1024
+us_status us_cache_store(const void* K, const void* V, const us_heads_layout* l, void* k_cache, void* v_cache, us_dtype cache_dt, long pages, long page,
+                         const int* table, long table_ld, const int* len, const int* count, long batch, long kv_heads, long s, long dh, void* stream);
+us_status us_attention_paged(const void* Q, long ldq, const void* k_cache, const void* v_cache, us_dtype cache_dt, long pages, long page, const int* table,
+                             long table_ld, const int* len, float* weights, void* O, long ldo, long batch, long heads, long kv_heads, long dh, long max_len,
+                             float alpha, void* workspace, size_t workspace_bytes, void* stream);
+size_t us_attention_paged_workspace_bytes(long batch, long heads, long kv_heads, long dh, long max_len, int with_weights);
+us_status us_cache_evict(void* k_cache, void* v_cache, float* weights, us_dtype cache_dt, long pages, long page, const int* table, long table_ld, const int* table_to,
+                         long table_to_ld, const int* len, int* new_len, int* kept, long batch, long kv_heads, long dh, long max_len, long keep, long recent,
+                         void* stream);
 
 #ifdef __cplusplus
 }

@@ -11,4 +11,5 @@ from .binding import (  # noqa: F401
     ffn_bias_workspace_bytes, softmax_fwd, softmax_bwd, softmax_xent, matmul_batched, attention_fwd, attention_bwd, sum_fwd, sum_bwd,
     FFN_KEEP8, GATE_GELU, GATE_RELU, GATE_SIGMOID, GATE_SILU, ROPE_HALVES, ROPE_NEIGHBOURS, ffn_gated_bwd, ffn_gated_fwd, ffn_gated_workspace_bytes, gate_scales, keep8_blocks, keep8_load,
     keep8_store, qk_norm_rope_bwd, qk_norm_rope_fwd, qk_norm_rope_workspace_bytes,
+    CACHE_PAGE_MAX, HeadsLayout, attention_cross_bwd, attention_cross_fwd, attention_cross_workspace_bytes, attention_paged, attention_paged_workspace_bytes, cache_evict, cache_store,
 )

@@ -21,12 +21,18 @@ HIST_BINS = 35
 GATE_SILU, GATE_GELU, GATE_RELU, GATE_SIGMOID = 0, 1, 2, 3
 FFN_KEEP8 = 4                       # mode bit of ffn_gated_fwd / ffn_gated_bwd, next to FFN_FP8
 ROPE_HALVES, ROPE_NEIGHBOURS = 0, 1
+CACHE_PAGE_MAX = 1024
 STATUS = {0: "US_OK", 1: "US_ERR_NULL", 2: "US_ERR_SHAPE", 3: "US_ERR_ALIGN", 4: "US_ERR_DTYPE",
           5: "US_ERR_WORKSPACE", 6: "US_ERR_LAUNCH", 7: "US_ERR_VALUE"}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libus_mi355x.so")
 _lib = None
+
+
+class HeadsLayout(ctypes.Structure):
+    """Where a tensor's heads lie: elements between batch items, heads and tokens (us_heads_layout in include/us.h)."""
+    _fields_ = [("batch", ctypes.c_long), ("head", ctypes.c_long), ("row", ctypes.c_long)]
 
 
 class UsError(RuntimeError):
@@ -110,7 +116,18 @@ def lib() -> ctypes.CDLL:
     L.us_qk_norm_rope_bwd.argtypes = [vp, l] + [vp] * 8 + [l, vp, vp] + [l] * 6 + [i, f, f, f, vp, sz, vp]
     L.us_qk_norm_rope_workspace_bytes.argtypes = [l] * 5
     L.us_qk_norm_rope_workspace_bytes.restype = sz
-    for name in ("us_gate_scales", "us_ffn_gated_fwd", "us_ffn_gated_bwd", "us_keep8_store", "us_keep8_load", "us_qk_norm_rope_fwd", "us_qk_norm_rope_bwd",
+    lp = ctypes.POINTER(HeadsLayout)
+    L.us_attention_cross_fwd.argtypes = [vp] * 6 + [l] * 6 + [f, lp, lp, lp, vp, sz, vp]
+    L.us_attention_cross_bwd.argtypes = [vp] * 10 + [l] * 6 + [f, f, f, lp, lp, lp, vp, sz, vp]
+    L.us_attention_cross_workspace_bytes.argtypes = [l] * 6
+    L.us_attention_cross_workspace_bytes.restype = sz
+    L.us_cache_store.argtypes = [vp, vp, lp, vp, vp, i, l, l, vp, l, vp, vp] + [l] * 4 + [vp]
+    L.us_attention_paged.argtypes = [vp, l, vp, vp, i, l, l, vp, l, vp, vp, vp] + [l] * 6 + [f, vp, sz, vp]
+    L.us_attention_paged_workspace_bytes.argtypes = [l] * 5 + [i]
+    L.us_attention_paged_workspace_bytes.restype = sz
+    L.us_cache_evict.argtypes = [vp, vp, vp, i, l, l, vp, l, vp, l, vp, vp, vp] + [l] * 6 + [vp]
+    for name in ("us_attention_cross_fwd", "us_attention_cross_bwd", "us_cache_store", "us_attention_paged", "us_cache_evict",
+                 "us_gate_scales", "us_ffn_gated_fwd", "us_ffn_gated_bwd", "us_keep8_store", "us_keep8_load", "us_qk_norm_rope_fwd", "us_qk_norm_rope_bwd",
                  "us_linear_scales", "us_cast_fp8", "us_cast_fp8_batch", "us_linear_fwd", "us_linear_bwd", "us_linear_bwd_noalloc", "us_gelu_fwd", "us_gelu_bwd",
                  "us_gelu_tables", "us_ffn_fwd", "us_ffn_bwd", "us_weighted_add", "us_ffn_res_fwd", "us_ffn_res_bwd", "us_act_fwd", "us_act_bwd", "us_layer_norm_fwd", "us_layer_norm_bwd", "us_exponent_histogram", "us_cast_snr",
                  "us_linear_bias_fwd", "us_bias_grad", "us_ffn_bias_fwd", "us_ffn_bias_bwd", "us_softmax_fwd", "us_softmax_bwd",
@@ -441,3 +458,52 @@ def qk_norm_rope_bwd(QKV, ld, wq, wk, pos, freq, dQ, dK, dV, dQKV, ld_d, dwq, dw
 
 def qk_norm_rope_workspace_bytes(batch: int, s: int, heads: int, kv_heads: int, dh: int) -> int:
     return int(lib().us_qk_norm_rope_workspace_bytes(batch, s, heads, kv_heads, dh))
+
+
+def attention_cross_fwd(Q, K, V, klen, O, lse, batch, heads, kv_heads, sq, sk, dh, alpha=0.0, lq=None, lkv=None, lo=None, workspace=None, workspace_bytes=0,
+                        stream=None):
+    """klen: int32 device pointer or None; lse: FP32, what the backward call reads, or None; lq, lkv, lo: HeadsLayout or None (one head after the other)."""
+    status = (_lib or lib()).us_attention_cross_fwd(Q, K, V, klen, O, lse, batch, heads, kv_heads, sq, sk, dh, alpha, lq, lkv, lo, workspace, workspace_bytes, stream)
+    if status:
+        raise UsError(status, "us_attention_cross_fwd")
+
+
+def attention_cross_bwd(Q, K, V, klen, O, lse, dO, dQ, dK, dV, batch, heads, kv_heads, sq, sk, dh, alpha=0.0, beta_q=0.0, beta_kv=0.0, lq=None, lkv=None, lo=None,
+                        workspace=None, workspace_bytes=0, stream=None):
+    status = (_lib or lib()).us_attention_cross_bwd(Q, K, V, klen, O, lse, dO, dQ, dK, dV, batch, heads, kv_heads, sq, sk, dh, alpha, beta_q, beta_kv, lq, lkv, lo,
+                                                    workspace, workspace_bytes, stream)
+    if status:
+        raise UsError(status, "us_attention_cross_bwd")
+
+
+def attention_cross_workspace_bytes(batch: int, heads: int, kv_heads: int, sq: int, sk: int, dh: int) -> int:
+    return int(lib().us_attention_cross_workspace_bytes(batch, heads, kv_heads, sq, sk, dh))
+
+
+def cache_store(K, V, layout, k_cache, v_cache, cache_dt, pages, page, table, table_ld, len, count, batch, kv_heads, s, dh, stream=None):
+    """len: int32 device pointer, the sequences' positions with the new tokens; count: how many of the s are new, or None: all."""
+    status = (_lib or lib()).us_cache_store(K, V, layout, k_cache, v_cache, cache_dt, pages, page, table, table_ld, len, count, batch, kv_heads, s, dh, stream)
+    if status:
+        raise UsError(status, "us_cache_store")
+
+
+def attention_paged(Q, ldq, k_cache, v_cache, cache_dt, pages, page, table, table_ld, len, weights, O, ldo, batch, heads, kv_heads, dh, max_len, alpha=0.0,
+                    workspace=None, workspace_bytes=0, stream=None):
+    """weights: FP32 [pages, kv_heads, page], added to, or None."""
+    status = (_lib or lib()).us_attention_paged(Q, ldq, k_cache, v_cache, cache_dt, pages, page, table, table_ld, len, weights, O, ldo, batch, heads, kv_heads, dh,
+                                                max_len, alpha, workspace, workspace_bytes, stream)
+    if status:
+        raise UsError(status, "us_attention_paged")
+
+
+def attention_paged_workspace_bytes(batch: int, heads: int, kv_heads: int, dh: int, max_len: int, with_weights: bool) -> int:
+    return int(lib().us_attention_paged_workspace_bytes(batch, heads, kv_heads, dh, max_len, int(with_weights)))
+
+
+def cache_evict(k_cache, v_cache, weights, cache_dt, pages, page, table, table_ld, table_to, table_to_ld, len, new_len, kept, batch, kv_heads, dh, max_len, keep,
+                recent, stream=None):
+    """table_to = table: in place.  kept: int32 [batch, kv_heads, keep], out; new_len: int32 [batch], out, or None."""
+    status = (_lib or lib()).us_cache_evict(k_cache, v_cache, weights, cache_dt, pages, page, table, table_ld, table_to, table_to_ld, len, new_len, kept, batch,
+                                            kv_heads, dh, max_len, keep, recent, stream)
+    if status:
+        raise UsError(status, "us_cache_evict")

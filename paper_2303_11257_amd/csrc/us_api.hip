@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <mutex>
+#include <utility>
 
 #include "us_device.h"
 #include "us_gate.h"
@@ -895,6 +896,163 @@ us_status us_qk_norm_rope_bwd(const void* QKV, long ld, const void* wq, const vo
   if (!(beta_wk > 0.0f)) beta_wk = (float)(1.0 / sqrt((double)batch * (double)s * (double)kv_heads));
   return from_hip(launch_heads_bwd(HeadsCall{QKV, wq, wk, pos, freq, ld, batch, s, heads, kv_heads, dh, rot, (int)pairs, eps}, dQ, dK, dV, dQKV, ld_d, dwq, dwk,
                                    beta_wq, beta_wk, workspace, as_stream(stream)));
+}
+
+// ---- attention over another sequence's keys --------------------------------------------------------------------------------------
+
+// (NULL: one head after the other)
+static us_heads_layout layout_of(const us_heads_layout* l, long heads, long s, long dh) { return l ? *l : us_heads_layout{heads * s * dh, s * dh, dh}; }
+static bool layout_ok(const us_heads_layout& l, long dh) {
+  return l.batch >= 0 && l.head >= 0 && l.row >= dh && l.row <= US_LAYOUT_ROW_MAX && l.batch % 8 == 0 && l.head % 8 == 0 && l.row % 8 == 0 &&
+         l.batch <= (1L << 48) && l.head <= (1L << 48);
+}
+// Whether no two of a written tensor's rows overlap: every dimension steps over all that the finer ones span.
+static bool layout_apart(const us_heads_layout& l, long batch, long heads, long s, long dh) {
+  long step[3] = {l.row, l.head, l.batch}, n[3] = {s, heads, batch}, span = dh;
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (step[j] < step[i]) {
+        std::swap(step[i], step[j]);
+        std::swap(n[i], n[j]);
+      }
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] < 2) continue;
+    if (step[i] < span) return false;
+    span += step[i] * (n[i] - 1);
+  }
+  return true;
+}
+
+static us_status cross_shape(long batch, long heads, long kv_heads, long sq, long sk, long dh) {
+  constexpr long kMost = 1L << 28;
+  if (batch < 0 || batch > 65535 || heads < 1 || heads > 65535 || kv_heads < 1 || heads % kv_heads != 0 || sq < 0 || sq > kMost || sk < 0 || sk > kMost) return US_ERR_SHAPE;
+  if (dh < 16 || dh > US_ROPE_HEAD_MAX || !mult16(dh)) return US_ERR_SHAPE;
+  // (workgroups are counted in 31 bits)
+  if (batch * heads * ((sq + 127) / 128) > (1L << 30) || batch * kv_heads * ((sk + 127) / 128) > (1L << 30)) return US_ERR_SHAPE;
+  return US_OK;
+}
+
+us_status us_attention_cross_fwd(const void* Q, const void* K, const void* V, const int* klen, void* O, float* lse, long batch, long heads, long kv_heads, long sq,
+                                 long sk, long dh, float alpha, const us_heads_layout* lq, const us_heads_layout* lkv, const us_heads_layout* lo, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  const CallScope scope(false);
+  if (us_status e = cross_shape(batch, heads, kv_heads, sq, sk, dh); e != US_OK) return e;
+  if (batch == 0 || sq == 0) return US_OK;
+  const CrossCall c{Q, K, V, klen, O, lse, nullptr, layout_of(lq, heads, sq, dh), layout_of(lkv, kv_heads, sk, dh), layout_of(lo, heads, sq, dh),
+                    batch, heads, kv_heads, sq, sk, dh, alpha};
+  if (!layout_ok(c.lq, dh) || (sk > 0 && !layout_ok(c.lkv, dh)) || !layout_ok(c.lo, dh) || !layout_apart(c.lo, batch, heads, sq, dh)) return US_ERR_SHAPE;
+  if (!Q || !O || (sk > 0 && (!K || !V))) return US_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(workspace) || ((uintptr_t)klen & 3) || ((uintptr_t)lse & 3)) return US_ERR_ALIGN;
+  if (workspace && workspace_bytes < cross_fwd_workspace_bytes(c)) return US_ERR_WORKSPACE;
+  return from_hip(launch_cross_fwd(c, workspace, as_stream(stream)));
+}
+
+us_status us_attention_cross_bwd(const void* Q, const void* K, const void* V, const int* klen, const void* O, const float* lse, const void* dO, void* dQ, void* dK,
+                                 void* dV, long batch, long heads, long kv_heads, long sq, long sk, long dh, float alpha, float beta_q, float beta_kv,
+                                 const us_heads_layout* lq, const us_heads_layout* lkv, const us_heads_layout* lo, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  const CallScope scope(false);
+  if (us_status e = cross_shape(batch, heads, kv_heads, sq, sk, dh); e != US_OK) return e;
+  if (batch == 0 || (sq == 0 && sk == 0)) return US_OK;
+  const CrossCall c{Q, K, V, klen, const_cast<void*>(O), const_cast<float*>(lse), dO, layout_of(lq, heads, sq, dh), layout_of(lkv, kv_heads, sk, dh),
+                    layout_of(lo, heads, sq, dh), batch, heads, kv_heads, sq, sk, dh, alpha};
+  if (sq > 0 && (!layout_ok(c.lq, dh) || !layout_ok(c.lo, dh) || !layout_apart(c.lq, batch, heads, sq, dh))) return US_ERR_SHAPE;
+  if (sk > 0 && (!layout_ok(c.lkv, dh) || !layout_apart(c.lkv, batch, kv_heads, sk, dh))) return US_ERR_SHAPE;
+  if ((sq > 0 && (!Q || !O || !lse || !dO || !dQ)) || (sk > 0 && (!K || !V || !dK || !dV))) return US_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(dO) || !aligned16(dQ) || !aligned16(dK) || !aligned16(dV) || !aligned16(workspace) ||
+      ((uintptr_t)klen & 3) || ((uintptr_t)lse & 3))
+    return US_ERR_ALIGN;
+  const size_t need = cross_bwd_workspace_bytes(c);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return US_ERR_WORKSPACE;
+  if (!(beta_q > 0.0f)) beta_q = 1.0f;
+  if (!(beta_kv > 0.0f)) beta_kv = sq > 0 ? (float)sqrt((double)sk / (double)sq * (double)kv_heads / (double)heads) : 1.0f;
+  return from_hip(launch_cross_bwd(c, dQ, dK, dV, beta_q, beta_kv, workspace, as_stream(stream)));
+}
+
+size_t us_attention_cross_workspace_bytes(long batch, long heads, long kv_heads, long sq, long sk, long dh) {
+  if (cross_shape(batch, heads, kv_heads, sq, sk, dh) != US_OK || batch == 0) return 0;
+  const CallScope scope(false);
+  CrossCall c{};
+  c.batch = batch; c.heads = heads; c.kv_heads = kv_heads;
+  c.sq = sq; c.sk = sk; c.dh = dh;
+  const size_t f = cross_fwd_workspace_bytes(c), b = cross_bwd_workspace_bytes(c);
+  return f > b ? f : b;
+}
+
+// ---- paged key-value cache ----------------------------------------------------------------------------------------------------------
+
+static us_status cache_shape(us_dtype dt, long pages, long page, long table_ld, long batch, long kv_heads, long dh) {
+  if (batch < 0 || batch > 65535 || kv_heads < 1 || kv_heads > 65535 || dh < 16 || dh > US_ROPE_HEAD_MAX || !mult16(dh)) return US_ERR_SHAPE;
+  if (page < 16 || page > US_CACHE_PAGE_MAX || (page & (page - 1)) != 0 || pages < 0 || pages > 0x7fffffffL || table_ld < 0 || table_ld > (1L << 28)) return US_ERR_SHAPE;
+  if (dt != US_F16 && dt != US_E4M3) return US_ERR_DTYPE;
+  return US_OK;
+}
+static CacheCall cache_call(const void* k, const void* v, us_dtype dt, long pages, long page, const int* table, long table_ld, long batch, long kv_heads, long dh) {
+  return CacheCall{const_cast<void*>(k), const_cast<void*>(v), dt == US_E4M3, pages, __builtin_ctzl((unsigned long)page), table, table_ld, batch, kv_heads, dh};
+}
+
+us_status us_cache_store(const void* K, const void* V, const us_heads_layout* l, void* k_cache, void* v_cache, us_dtype cache_dt, long pages, long page,
+                         const int* table, long table_ld, const int* len, const int* count, long batch, long kv_heads, long s, long dh, void* stream) {
+  const CallScope scope(false);
+  if (us_status e = cache_shape(cache_dt, pages, page, table_ld, batch, kv_heads, dh); e != US_OK) return e;
+  if (s < 0 || s > (1L << 30)) return US_ERR_SHAPE;
+  if (batch == 0 || s == 0 || pages == 0 || table_ld == 0) return US_OK;
+  const us_heads_layout layout = layout_of(l, kv_heads, s, dh);
+  if (!layout_ok(layout, dh)) return US_ERR_SHAPE;
+  if (!K || !V || !k_cache || !v_cache || !table || !len) return US_ERR_NULL;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(k_cache) || !aligned16(v_cache) || ((uintptr_t)table & 3) || ((uintptr_t)len & 3) || ((uintptr_t)count & 3))
+    return US_ERR_ALIGN;
+  return from_hip(launch_cache_store(cache_call(k_cache, v_cache, cache_dt, pages, page, table, table_ld, batch, kv_heads, dh), K, V, layout, len, count, s, as_stream(stream)));
+}
+
+static us_status paged_shape(long batch, long heads, long kv_heads, long dh, long max_len) {
+  if (heads < 1 || heads > 65535 || heads % kv_heads != 0 || max_len < 0 || max_len > (1L << 30)) return US_ERR_SHAPE;
+  // (workgroups are counted in 31 bits)
+  if (batch * heads > (1L << 28) || batch * kv_heads * ((max_len + 255) / 256) > (1L << 30)) return US_ERR_SHAPE;
+  return US_OK;
+}
+
+us_status us_attention_paged(const void* Q, long ldq, const void* k_cache, const void* v_cache, us_dtype cache_dt, long pages, long page, const int* table,
+                             long table_ld, const int* len, float* weights, void* O, long ldo, long batch, long heads, long kv_heads, long dh, long max_len,
+                             float alpha, void* workspace, size_t workspace_bytes, void* stream) {
+  const CallScope scope(false);
+  if (us_status e = cache_shape(cache_dt, pages, page, table_ld, batch, kv_heads, dh); e != US_OK) return e;
+  if (us_status e = paged_shape(batch, heads, kv_heads, dh, max_len); e != US_OK) return e;
+  if (ldq < heads * dh || ldq % 8 != 0 || ldo < heads * dh || ldo % 8 != 0) return US_ERR_SHAPE;
+  if (batch == 0) return US_OK;
+  const bool any = pages > 0 && table_ld > 0 && max_len > 0;
+  if (!Q || !O || (any && (!k_cache || !v_cache || !table || !len))) return US_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(O) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(workspace) || ((uintptr_t)table & 3) || ((uintptr_t)len & 3) ||
+      ((uintptr_t)weights & 3))
+    return US_ERR_ALIGN;
+  const size_t need = paged_workspace_bytes(batch, heads, kv_heads, dh, max_len, weights != nullptr);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return US_ERR_WORKSPACE;
+  return from_hip(launch_paged(PagedCall{cache_call(k_cache, v_cache, cache_dt, pages, page, table, any ? table_ld : 0, batch, kv_heads, dh), Q, ldq, len, weights, O, ldo,
+                                         batch, heads, kv_heads, dh, max_len, alpha},
+                               workspace, as_stream(stream)));
+}
+
+size_t us_attention_paged_workspace_bytes(long batch, long heads, long kv_heads, long dh, long max_len, int with_weights) {
+  if (batch < 1 || kv_heads < 1 || dh < 1 || paged_shape(batch, heads, kv_heads, dh, max_len) != US_OK) return 0;
+  const CallScope scope(false);
+  return paged_workspace_bytes(batch, heads, kv_heads, dh, max_len, with_weights != 0);
+}
+
+us_status us_cache_evict(void* k_cache, void* v_cache, float* weights, us_dtype cache_dt, long pages, long page, const int* table, long table_ld, const int* table_to,
+                         long table_to_ld, const int* len, int* new_len, int* kept, long batch, long kv_heads, long dh, long max_len, long keep, long recent,
+                         void* stream) {
+  const CallScope scope(false);
+  if (us_status e = cache_shape(cache_dt, pages, page, table_ld, batch, kv_heads, dh); e != US_OK) return e;
+  if (max_len < 0 || max_len > (1L << 30) || keep < 0 || keep > (1L << 30) || recent < 0 || recent > keep || table_to_ld < 0 || table_to_ld > (1L << 28)) return US_ERR_SHAPE;
+  if (table_to == table && table_to_ld != table_ld) return US_ERR_SHAPE;
+  if (batch == 0) return US_OK;
+  if (!len || (keep > 0 && (!k_cache || !v_cache || !weights || !table || !table_to || !kept))) return US_ERR_NULL;
+  if (!aligned16(k_cache) || !aligned16(v_cache) || ((uintptr_t)weights & 3) || ((uintptr_t)table & 3) || ((uintptr_t)table_to & 3) || ((uintptr_t)len & 3) ||
+      ((uintptr_t)new_len & 3) || ((uintptr_t)kept & 3))
+    return US_ERR_ALIGN;
+  const long most = max_len < table_ld * page ? max_len : table_ld * page;
+  return from_hip(launch_cache_evict(cache_call(k_cache, v_cache, cache_dt, pages, page, table, table_ld, batch, kv_heads, dh), weights, table_to, table_to_ld, len, new_len,
+                                     kept, most, keep, recent, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -20,8 +20,8 @@ thread_local int g_note_count = 0;
 thread_local char g_record[1024];
 }  // namespace
 
-CallScope::CallScope() : outer(g_call_device) {
-  g_note_count = 0;
+CallScope::CallScope(bool matmul) : outer(g_call_device) {
+  if (matmul) g_note_count = 0;
   g_call_device = kNotAsked;
 }
 CallScope::~CallScope() { g_call_device = outer; }

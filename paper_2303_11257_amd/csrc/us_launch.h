@@ -24,10 +24,10 @@ const DeviceInfo& device_info();
 
 // For the time of one call of an entry point that chooses among kernels: clears the calling thread's launch record, and asks for
 // the current device once, at the first of the dozen places that want to know something about it (0.05 us each): a call that is refused or
-// has nothing to do asks the runtime nothing, which would start it up in a process that may still fork.
+// has nothing to do asks the runtime nothing, which would start it up in a process that may still fork.  matmul = false: a call that the record leaves out.
 struct CallScope {
   int outer;
-  CallScope();
+  explicit CallScope(bool matmul = true);
   ~CallScope();
   CallScope(const CallScope&) = delete;
   CallScope& operator=(const CallScope&) = delete;
@@ -116,6 +116,46 @@ size_t heads_workspace_bytes(long tokens, long dh);
 hipError_t launch_heads_fwd(const HeadsCall& c, void* Q, void* K, void* V, hipStream_t stream);
 hipError_t launch_heads_bwd(const HeadsCall& c, const void* dQ, const void* dK, const void* dV, void* dQKV, long ld_dx, void* dwq, void* dwk,
                             float beta_wq, float beta_wk, void* workspace, hipStream_t stream);
+
+// Attention over another sequence's keys (us_cross.hip).
+struct CrossCall {
+  const void *Q, *K, *V;
+  const int* klen;
+  void* O;
+  float* lse;
+  const void* dO;
+  us_heads_layout lq, lkv, lo;
+  long batch, heads, kv_heads, sq, sk, dh;
+  float alpha;
+};
+size_t cross_fwd_workspace_bytes(const CrossCall& c);
+size_t cross_bwd_workspace_bytes(const CrossCall& c);
+hipError_t launch_cross_fwd(const CrossCall& c, void* workspace, hipStream_t stream);      // workspace may be NULL
+hipError_t launch_cross_bwd(const CrossCall& c, void* dQ, void* dK, void* dV, float beta_q, float beta_kv, void* workspace, hipStream_t stream);
+
+// A paged key-value cache (us_cache.hip), and attention of one token over it (us_paged.hip).
+struct CacheCall {
+  void *k, *v;
+  bool fp8;
+  long pages;
+  int shift;               // log2 of a page's positions
+  const int* table;
+  long table_ld, batch, kv_heads, dh;
+};
+struct PagedCall {
+  CacheCall cache;
+  const void* Q;
+  long ldq;
+  const int* len;
+  void *weights, *O;
+  long ldo, batch, heads, kv_heads, dh, max_len;
+  float alpha;
+};
+size_t paged_workspace_bytes(long batch, long heads, long kv, long dh, long most, bool weights);
+hipError_t launch_paged(const PagedCall& c, void* workspace, hipStream_t stream);
+hipError_t launch_cache_store(const CacheCall& c, const void* K, const void* V, const us_heads_layout& l, const int* len, const int* count, long s, hipStream_t stream);
+hipError_t launch_cache_evict(const CacheCall& c, float* weights, const int* table_to, long table_to_ld, const int* len, int* new_len, int* kept, long max_len, long keep,
+                              long recent, hipStream_t stream);
 
 size_t bias_grad_workspace_bytes(long b, long n);
 hipError_t launch_bias_grad(const void* G, us_dtype g_dt, void* dc, long b, long n, float beta, void* workspace, hipStream_t stream);
