@@ -585,7 +585,7 @@ size_t us_attention_cross_workspace_bytes(long batch, long heads, long kv_heads,
  *   table_to == table: in place; the slots behind are left as they were, and a page must belong to one sequence only.  Another table_to (int32
  *   [batch, table_to_ld], pages of the same pools that hold none of the sequences): the kept rows are copied there.
  *   new_len[b] = min(len[b], keep) (int32 [batch], may be len itself, or NULL), kept: int32 [batch, kv_heads, keep], the positions that were kept, -1 behind a shorter
- *   sequence's.  0 <= recent <= keep.  max_len as above.
+ *   sequence's.  0 <= recent <= keep <= 2^20.  max_len as above.
  *
  * dh a multiple of 16 up to US_ROPE_HEAD_MAX; batch and heads up to 65535.  All pools and rows 16-byte aligned.  Results do not depend on scheduling.
  */

@@ -995,7 +995,8 @@ us_status us_cache_store(const void* K, const void* V, const us_heads_layout* l,
                          const int* table, long table_ld, const int* len, const int* count, long batch, long kv_heads, long s, long dh, void* stream) {
   const CallScope scope(false);
   if (us_status e = cache_shape(cache_dt, pages, page, table_ld, batch, kv_heads, dh); e != US_OK) return e;
-  if (s < 0 || s > (1L << 30)) return US_ERR_SHAPE;
+  // (a sequence's 16-byte pieces are counted in 31 bits)
+  if (s < 0 || s > (1L << 30) || s * kv_heads * (dh / 8) > 0x7fffffffL) return US_ERR_SHAPE;
   if (batch == 0 || s == 0 || pages == 0 || table_ld == 0) return US_OK;
   const us_heads_layout layout = layout_of(l, kv_heads, s, dh);
   if (!layout_ok(layout, dh)) return US_ERR_SHAPE;
@@ -1045,6 +1046,8 @@ us_status us_cache_evict(void* k_cache, void* v_cache, float* weights, us_dtype 
   if (us_status e = cache_shape(cache_dt, pages, page, table_ld, batch, kv_heads, dh); e != US_OK) return e;
   if (max_len < 0 || max_len > (1L << 30) || keep < 0 || keep > (1L << 30) || recent < 0 || recent > keep || table_to_ld < 0 || table_to_ld > (1L << 28)) return US_ERR_SHAPE;
   if (table_to == table && table_to_ld != table_ld) return US_ERR_SHAPE;
+  // (workgroups are counted in 31 bits, parts of a sequence in 16)
+  if (batch * kv_heads > (1L << 28) || keep > (1L << 20)) return US_ERR_SHAPE;
   if (batch == 0) return US_OK;
   if (!len || (keep > 0 && (!k_cache || !v_cache || !weights || !table || !table_to || !kept))) return US_ERR_NULL;
   if (!aligned16(k_cache) || !aligned16(v_cache) || ((uintptr_t)weights & 3) || ((uintptr_t)table & 3) || ((uintptr_t)table_to & 3) || ((uintptr_t)len & 3) ||

@@ -18,6 +18,22 @@ typedef _Float16 v4h __attribute__((ext_vector_type(4)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
+// Division of an unsigned 32-bit number by a divisor that the host knows (Granlund & Montgomery, round-up method): one high
+// multiplication and three shifts and additions of scalars, where the compiler's division of two runtime integers is a chain
+// of about twenty dependent scalar and vector instructions through a floating-point reciprocal.
+struct FastDiv {
+  uint32_t mul, pre, post;
+  static FastDiv by(uint32_t d) {                                          // 1 <= d < 2^31
+    uint32_t l = 0;
+    while ((1u << l) < d) ++l;                                             // ceil(log2 d)
+    return {(uint32_t)((((uint64_t)1 << 32) * ((1u << l) - d)) / d + 1), l < 1 ? l : 1, l > 1 ? l - 1 : 0};
+  }
+  __host__ __device__ __forceinline__ uint32_t of(uint32_t n) const {
+    const uint32_t t = (uint32_t)(((uint64_t)mul * n) >> 32);
+    return (t + ((n - t) >> pre)) >> post;
+  }
+};
+
 // Unit-scaling factors of gelu(x) = x*Phi(x) for x ~ N(0,1) (Table A.2 prints 1.701 / 1.481):
 // alpha = 1/std(gelu), beta = 1/rms(gelu'), closed forms
 //   E[gelu^2] = 1/3 + 1/(2 pi sqrt3), E[gelu] = 1/(2 sqrt pi), E[gelu'^2] = 1/3 + 2/(3 pi sqrt3).

@@ -57,6 +57,12 @@ struct RowTile {
   }
 };
 
+// 16 bytes per lane straight to LDS, lane after lane from `lds` on; zeros where the offset lies beyond the resource.  (A function of its own: from inside a lambda
+// that a kernel template calls, the compiler's host pass leaves out the kernel's stub.)
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t* lds, int off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, US_LDS_AT(void, lds), 16, off, 0, 0, 0);
+}
+
 // The loads of a tile of ROWS rows by THREADS threads, straight to LDS; rows from `rows` on and columns from dh on are zeros.
 template <int NB, int ROWS, int THREADS>
 struct TileLoads {
@@ -76,7 +82,7 @@ struct TileLoads {
 #pragma unroll
     for (int j = 0; j < LD; ++j)
       if (BYTES / 16 % THREADS == 0 || j * THREADS + wave * 64 < BYTES / 16)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(res, US_LDS_AT(void, lds + (j * THREADS + wave * 64) * 16), 16, (int)off[j], 0, 0, 0);
+        load_to_lds(res, lds + (j * THREADS + wave * 64) * 16, (int)off[j]);
   }
 };
 

@@ -19,22 +19,6 @@ enum GemmEpi : int {
   EPI_RESIDUAL = 7, EPI_GATE = 10, EPI_GATE8 = 11, EPI_GATE_GRAD = 12, EPI_GATE8_GRAD = 13
 };
 
-// Division of an unsigned 32-bit number by a divisor that the host knows (Granlund & Montgomery, round-up method): one high
-// multiplication and three shifts and additions of scalars, where the compiler's division of two runtime integers is a chain
-// of about twenty dependent scalar and vector instructions through a floating-point reciprocal.
-struct FastDiv {
-  uint32_t mul, pre, post;
-  static FastDiv by(uint32_t d) {                                          // 1 <= d < 2^31
-    uint32_t l = 0;
-    while ((1u << l) < d) ++l;                                             // ceil(log2 d)
-    return {(uint32_t)((((uint64_t)1 << 32) * ((1u << l) - d)) / d + 1), l < 1 ? l : 1, l > 1 ? l - 1 : 0};
-  }
-  __host__ __device__ __forceinline__ uint32_t of(uint32_t n) const {
-    const uint32_t t = (uint32_t)(((uint64_t)mul * n) >> 32);
-    return (t + ((n - t) >> pre)) >> post;
-  }
-};
-
 // ---- workgroup -> output tile ------------------------------------------------------------------------
 // Workgroups are handed to the device's XCDs round-robin by linear id, and every XCD has its own L2.  When
 // the tile grid divides evenly (choose_xcd_grid), XCD x gets a compact rectangle of

@@ -21,6 +21,8 @@ struct Pages {
   float* scores;            // [batch * heads][score_ld], base 2, if weights are wanted
   long score_ld, table_ld, pages;
   int shift;                // log2 of the positions of a page
+  FastDiv by_groups, by_tiles, by_kv, by_rep;
+  uint32_t groups;          // workgroups of a part
 };
 
 __device__ __forceinline__ v4f mfma16(v8h a, v8h b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -40,25 +42,123 @@ __device__ __forceinline__ float row_reduce(float v, F f) {
   return halves(f(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)), f);
 }
 
+// A tile of values in LDS: rows of P bytes, 16-byte chunk c at c ^ swz(row).  The 32 lanes that a transposing read serves together touch 32 bytes in each of eight
+// neighbouring rows (FP16), or 16 bytes in each of those and of the eight rows that lie 16 further on (codes): every bank once.
+template <int NB, bool FP8>
+struct ValueTile {
+  static constexpr int P = FP8 ? (NB <= 2 ? 64 : NB <= 4 ? 128 : 256) : RowTile<NB>::P;
+  static constexpr int LOADS = P / 64;      // of 16 rows by a wave
+  __device__ __forceinline__ static int swz(int row) {
+    if (FP8) {
+      if (P == 64) return ((row >> 2) & 1) | ((row >> 4) & 1) << 1;
+      if (P == 128) return ((row >> 1) & 3) | ((row >> 4) & 1) << 2;
+      return (row & 7) | ((row >> 4) & 1) << 3;
+    }
+    if (P == 64) return ((row >> 2) & 1) << 1;
+    if (P == 128) return ((row >> 1) & 3) << 1;
+    return (row & 7) << 1;
+  }
+};
+
+// A wave's keys of 32 positions, and whether their two sixteens are there.
+template <int UNITS>
+struct KeyTile {
+  v4i k[2][UNITS];
+  bool there0, there1;
+};
+
+// s_waitcnt vmcnt(N), and nothing that reads memory moves across it
+template <int N>
+__device__ __forceinline__ void wait_newest() {
+  static_assert(N >= 0 && N < 64, "");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 template <int NB, bool FP8, bool PAGED>
 __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(AttendArgs a, Pages pg) {
-  using T = RowTile<NB>;
+  using T = ValueTile<NB, FP8>;
   constexpr int ES = FP8 ? 1 : 2, UNITS = FP8 ? (NB + 1) / 2 : NB;      // 16-byte chunks of a key per lane
-  constexpr int CPR = FP8 ? 2 * NB : 4 * NB, VL = kStep * CPR / 64;     // ... of a row of values, and a lane's share of a tile
+  constexpr int VL = T::LOADS, REQUEST = 2 * (VL + UNITS);              // loads of a tile
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x & 63, l16 = lane & 15, l4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nrows = a.sq * a.rep;
-  const int split = (int)(blockIdx.x % a.splits), rb = (int)(blockIdx.x / a.splits % a.tiles);
-  const long group = blockIdx.x / a.splits / a.tiles;
-  const int b = (int)(group / a.kv), kvh = (int)(group % a.kv);
+  // (the parts come last: workgroups go to the XCDs in turn, and one that got the same part of every sequence would have all the short ones' idle parts, or none:
+  // 48 sequences of up to 4096 positions in eight parts of their own 112 us, this way 92)
+  const uint32_t split = pg.by_groups.of(blockIdx.x);
+  const uint32_t i0 = blockIdx.x - split * pg.groups, group = pg.by_tiles.of(i0);
+  const int rb = (int)(i0 - group * a.tiles);
+  const int b = (int)pg.by_kv.of(group), kvh = (int)(group - (uint32_t)b * a.kv);
   const int n = a.keys_of(b);
-  const int begin = split * a.per_split, end = begin + a.per_split < n ? begin + a.per_split : n;
-  const int r0 = rb * 16 + l16, token = r0 / a.rep, head = kvh * a.rep + (r0 - token * a.rep);
+  const int begin = (int)split * a.per_split, end = begin + a.per_split < n ? begin + a.per_split : n;
+  const int r0 = rb * 16 + l16, token = (int)pg.by_rep.of((uint32_t)r0), head = kvh * a.rep + (r0 - token * a.rep);
   const bool on = r0 < nrows;
-  uint8_t* vt = lds + wave * kStep * T::P;
+  uint8_t* const tiles = lds + wave * 2 * kStep * T::P;
 
-  // the rows' fragments; the columns that a lane's chunk of a key holds
+  const long row_bytes = PAGED ? (long)a.dh * ES : a.k.row;
+  // where the 16 positions at `pos` start, in rows: -1 beyond the end, or on a page that there is not
+  auto block_of = [&](int pos) -> long {
+    if (pos >= end) return -1;
+    if constexpr (PAGED) {
+      const int page = pg.table[(long)b * pg.table_ld + (pos >> pg.shift)];
+      if (page < 0 || page >= pg.pages) return -1;
+      return (((long)page * a.kv + kvh) << pg.shift) + (pos & ((1 << pg.shift) - 1));
+    } else {
+      return pos;
+    }
+  };
+  const uint8_t* kbase = PAGED ? pg.k : (const uint8_t*)(a.k.p + b * a.k.batch + kvh * a.k.head);
+  const uint8_t* vbase = PAGED ? pg.v : (const uint8_t*)(a.v.p + b * a.v.batch + kvh * a.v.head);
+  // a lane's chunks of a block of 16 positions: of its key, and of the values on their way to LDS; beyond the head's columns nothing (zeros)
+  constexpr int kNowhere = 0x7ffffff0;
+  int koff[UNITS], voff[FP8 ? 2 : 1][VL];
+#pragma unroll
+  for (int t = 0; t < UNITS; ++t) {
+    const int byte = (4 * t + l4) * 16;
+    koff[t] = byte < a.dh * ES ? l16 * (int)row_bytes + byte : kNowhere;
+  }
+#pragma unroll
+  for (int i = 0; i < (FP8 ? 2 : 1); ++i)
+#pragma unroll
+    for (int j = 0; j < VL; ++j) {
+      const int o = (j * 64 + lane) * 16, row = o / T::P, byte = (o % T::P) ^ (T::swz(row + 16 * i) << 4);
+      voff[i][j] = byte < a.dh * ES ? row * (int)row_bytes + byte : kNowhere;
+    }
+
+  // A tile on its way, requested while its predecessor is computed: the values first, so that they have landed when the keys are there.
+  using Tile = KeyTile<UNITS>;
+  auto request = [&](Tile& x, uint8_t* vt, int pos, long at0, long at1) {
+    x.there0 = at0 >= 0;
+    x.there1 = at1 >= 0;
+    auto bytes = [&](int from, long at) -> int {
+      const int rows = end - from < 16 ? end - from : 16;
+      return at < 0 || rows <= 0 ? 0 : (rows - 1) * (int)row_bytes + a.dh * ES;
+    };
+    const int bytes0 = bytes(pos, at0), bytes1 = bytes(pos + 16, at1);
+    const long o0 = at0 < 0 ? 0 : at0 * row_bytes, o1 = at1 < 0 ? 0 : at1 * row_bytes;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc((void*)(vbase + (i ? o1 : o0)), 0, i ? bytes1 : bytes0, 0x00027000);
+#pragma unroll
+      for (int j = 0; j < VL; ++j)
+        load_to_lds(res, vt + i * 16 * T::P + j * 1024, voff[FP8 ? i : 0][j]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc((void*)(kbase + (i ? o1 : o0)), 0, i ? bytes1 : bytes0, 0x00027000);
+#pragma unroll
+      for (int t = 0; t < UNITS; ++t) x.k[i][t] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(res, koff[t], 0, 0));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr int kRound = kWaves * kStep;
+  Tile tile[2];
+  int pos = begin + wave * kStep;
+  if (pos < end) request(tile[0], tiles, pos, block_of(pos), block_of(pos + 16));
+  long n0 = block_of(pos + kRound), n1 = block_of(pos + kRound + 16);
+
+  // the rows' fragments: the columns that a lane's chunk of a key holds
   v8h qf[FP8 ? 2 * UNITS : UNITS];
   {
     const _Float16* q = (const _Float16*)((const uint8_t*)(a.q.p + b * a.q.batch + head * a.q.head) + (long)token * a.q.row);
@@ -69,47 +169,11 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
       if (on && col < a.dh) qf[t] = *reinterpret_cast<const v8h*>(q + col);
     }
   }
-  const v4i zero4 = {0, 0, 0, 0};
-  const long row_bytes = PAGED ? (long)a.dh * ES : a.k.row;
-  // the base of the 16 positions at `pos`, or NULL: beyond the end, or on a page that there is not
-  auto block_of = [&](int pos, const uint8_t* base) -> const uint8_t* {
-    if (pos >= end) return nullptr;
-    if constexpr (PAGED) {
-      const int page = pg.table[(long)b * pg.table_ld + (pos >> pg.shift)];
-      if (page < 0 || page >= pg.pages) return nullptr;
-      return base + ((((long)page * a.kv + kvh) << pg.shift) + (pos & ((1 << pg.shift) - 1))) * row_bytes;
-    } else {
-      return base + (long)pos * row_bytes;
-    }
-  };
-  const uint8_t* kbase = PAGED ? pg.k : (const uint8_t*)(a.k.p + b * a.k.batch + kvh * a.k.head);
-  const uint8_t* vbase = PAGED ? pg.v : (const uint8_t*)(a.v.p + b * a.v.batch + kvh * a.v.head);
-
   v4f acc[2 * NB];
 #pragma unroll
   for (int j = 0; j < 2 * NB; ++j) acc[j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   float m = -__builtin_inff(), sum = 0.0f;
-  for (int pos = begin + wave * kStep; pos < end; pos += kWaves * kStep) {
-    const uint8_t *k0 = block_of(pos, kbase), *k1 = block_of(pos + 16, kbase), *v0 = block_of(pos, vbase), *v1 = block_of(pos + 16, vbase);
-    v4i kr[2][UNITS], vr[VL];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint8_t* at = i ? k1 : k0;
-      const bool live = at && pos + 16 * i + l16 < end;
-#pragma unroll
-      for (int t = 0; t < UNITS; ++t) {
-        const int byte = (4 * t + l4) * 16;
-        kr[i][t] = zero4;
-        if (live && byte < a.dh * ES) kr[i][t] = *reinterpret_cast<const v4i*>(at + l16 * row_bytes + byte);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < VL; ++j) {
-      const int x = j * 64 + lane, row = x / CPR, byte = (x - row * CPR) * 16;
-      const uint8_t* at = row < 16 ? v0 : v1;
-      vr[j] = zero4;
-      if (at && pos + row < end && byte < a.dh * ES) vr[j] = *reinterpret_cast<const v4i*>(at + (row & 15) * row_bytes + byte);
-    }
+  auto compute = [&](const Tile& x, const uint8_t* vt, int pos, bool newer) {
     // scores of 2 x 16 positions: a lane holds its row's 4 l4 .. + 3 of either
     v4f s[2];
     float top = -__builtin_inff();
@@ -119,17 +183,16 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
 #pragma unroll
       for (int t = 0; t < UNITS; ++t) {
         if constexpr (FP8) {
-          s[i] = mfma16(codes8(kr[i][t][0], kr[i][t][1]), qf[2 * t], s[i]);
-          s[i] = mfma16(codes8(kr[i][t][2], kr[i][t][3]), qf[2 * t + 1], s[i]);
+          s[i] = mfma16(codes8(x.k[i][t][0], x.k[i][t][1]), qf[2 * t], s[i]);
+          s[i] = mfma16(codes8(x.k[i][t][2], x.k[i][t][3]), qf[2 * t + 1], s[i]);
         } else {
-          s[i] = mfma16(__builtin_bit_cast(v8h, kr[i][t]), qf[t], s[i]);
+          s[i] = mfma16(__builtin_bit_cast(v8h, x.k[i][t]), qf[t], s[i]);
         }
       }
-      const bool there = i ? k1 != nullptr : k0 != nullptr;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         s[i][e] *= a.c2;
-        if (!there || pos + 16 * i + 4 * l4 + e >= end) s[i][e] = -__builtin_inff();
+        if (!(i ? x.there1 : x.there0) || pos + 16 * i + 4 * l4 + e >= end) s[i][e] = -__builtin_inff();
         top = __builtin_fmaxf(top, s[i][e]);
       }
       if (PAGED && pg.scores && on && pos + 16 * i < end)
@@ -138,44 +201,58 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
     top = __builtin_fmaxf(m, row_reduce(top, [](float x, float y) { return __builtin_fmaxf(x, y); }));
     // (positions that are all on pages that there are not: nothing is there yet)
     const float use = top == -__builtin_inff() ? 0.0f : top;
-    const float f = __builtin_amdgcn_exp2f(m - use);
+    if (__builtin_amdgcn_ballot_w64(top > m)) {
+      const float f = __builtin_amdgcn_exp2f(m - use);
+      sum *= f;
+#pragma unroll
+      for (int j = 0; j < 2 * NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][e] *= f;
+    }
     m = top;
-    sum *= f;
-#pragma unroll
-    for (int j = 0; j < 2 * NB; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[j][e] *= f;
     v8h p;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f(s[i][e] - use);
-        sum += x;
-        p[4 * i + e] = (_Float16)x;
+        const float y = __builtin_amdgcn_exp2f(s[i][e] - use);
+        sum += y;
+        p[4 * i + e] = (_Float16)y;
       }
-    // the values through LDS, which only this wave uses
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int j = 0; j < VL; ++j) {
-      const int x = j * 64 + lane, row = x / CPR, chunk = x - row * CPR;
-      uint8_t* to = vt + row * T::P;
-      if constexpr (FP8) {
-        *US_LDS_AT(v8h, to + (((2 * chunk) ^ T::swz(row)) << 4)) = codes8(vr[j][0], vr[j][1]);
-        *US_LDS_AT(v8h, to + (((2 * chunk + 1) ^ T::swz(row)) << 4)) = codes8(vr[j][2], vr[j][3]);
-      } else {
-        *US_LDS_AT(v4i, to + ((chunk ^ T::swz(row)) << 4)) = vr[j];
-      }
-    }
-    __builtin_amdgcn_wave_barrier();
+    // the values have landed: what may still be on its way is the next tile
+    if (newer) wait_newest<REQUEST>();
+    else wait_newest<0>();
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < 2 * NB; ++j) {
       // lane: column 16 j + l16, positions 4 l4 .. + 3 of either sixteen
-      const int row = 4 * l4 + (l16 >> 2), chunk = 2 * j + ((l16 & 3) >> 1);
-      const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(US_LDS_AT(v4s, vt + row * T::P + ((chunk ^ T::swz(row)) << 4) + (l16 & 1) * 8));
-      const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(US_LDS_AT(v4s, vt + (row + 16) * T::P + ((chunk ^ T::swz(row + 16)) << 4) + (l16 & 1) * 8));
-      struct { v4s x, y; } both = {x, y};
-      acc[j] = mfma16(__builtin_bit_cast(v8h, both), p, acc[j]);
+      if constexpr (FP8) {
+        const int row = (l16 >> 3) * 16 + 4 * l4 + ((l16 >> 1) & 3);
+        const v2i c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(US_LDS_AT(v2i, vt + row * T::P + ((j ^ T::swz(row)) << 4) + (l16 & 1) * 8));
+        acc[j] = mfma16(codes8(c[0], c[1]), p, acc[j]);
+      } else {
+        const int row = 4 * l4 + (l16 >> 2), chunk = 2 * j + ((l16 & 3) >> 1);
+        const uint8_t* at = vt + row * T::P + ((chunk ^ T::swz(row)) << 4) + (l16 & 1) * 8;      // (16 rows on: the same swizzle)
+        const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(US_LDS_AT(v4s, at));
+        const v4s z = __builtin_amdgcn_ds_read_tr16_b64_v4i16(US_LDS_AT(v4s, at + 16 * T::P));
+        struct { v4s y, z; } both = {y, z};
+        acc[j] = mfma16(__builtin_bit_cast(v8h, both), p, acc[j]);
+      }
+    }
+    // (the next request to this half of LDS comes after these reads have been used)
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  for (; pos < end; pos += 2 * kRound) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = pos + h * kRound;
+      if (at >= end) break;
+      const bool newer = at + kRound < end;
+      if (newer) request(tile[h ^ 1], tiles + (h ^ 1) * kStep * T::P, at + kRound, n0, n1);
+      n0 = block_of(at + 2 * kRound);
+      n1 = block_of(at + 2 * kRound + 16);
+      compute(tile[h], tiles + h * kStep * T::P, at, newer);
     }
   }
   sum = row_reduce(sum, [](float x, float y) { return x + y; });
@@ -224,34 +301,91 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
   }
 }
 
-// weights of 256 positions of a key head: += sum over its rows of 2^(s - m) / l, m and l joined from the parts
-__global__ void __launch_bounds__(kThreads) weights_kernel(AttendArgs a, Pages pg, int segments) {
-  __shared__ float ms[64], inv[64];
-  const int seg = (int)(blockIdx.x % segments);
-  const long group = blockIdx.x / segments;
-  const int b = (int)(group / a.kv), kvh = (int)(group % a.kv);
-  const int n = a.keys_of(b), pos = seg * kThreads + (int)threadIdx.x;
-  if (seg * kThreads >= n) return;
+// What is left when all parts are there.  The first `joins` workgroups join a row each: O = a sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s (parts without
+// positions have l_s = 0 and are not read); the others add the weights of 256 positions of a key head: sum over its rows of 2^(score - m) / l.
+constexpr int kMostParts = 1024;
+__global__ void __launch_bounds__(kThreads) finish_kernel(AttendArgs a, Pages pg, long joins, int segments) {
+  const int tid = (int)threadIdx.x;
   const long stride = a.part_stride / a.dh;
-  float w = 0.0f;
+  __shared__ float fs[kMostParts];
+  __shared__ __attribute__((aligned(16))) float red[kThreads * 4];
+  if ((long)blockIdx.x < joins) {
+    const long row = blockIdx.x, bh = row / a.sq;
+    const int q = (int)(row - bh * a.sq), b = (int)(bh / a.heads), head = (int)(bh - (long)b * a.heads);
+    float m = -__builtin_inff(), sum = 0.0f;
+    float2 st[kMostParts / kThreads];
+#pragma unroll
+    for (int i = 0; i < kMostParts / kThreads; ++i) {
+      st[i] = make_float2(-__builtin_inff(), 0.0f);
+      if (tid + i * kThreads < a.splits) st[i] = a.stats[(tid + i * kThreads) * stride + row];
+      m = __builtin_fmaxf(m, st[i].x);
+    }
+    red[tid] = wave_max(m);
+    __syncthreads();
+    m = __builtin_fmaxf(__builtin_fmaxf(red[0], red[64]), __builtin_fmaxf(red[128], red[192]));
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMostParts / kThreads; ++i) {
+      const float f = st[i].y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(st[i].x - m);      // (a NaN sum is not zero)
+      if (tid + i * kThreads < a.splits) fs[tid + i * kThreads] = f;
+      if (st[i].y != 0.0f) sum = __builtin_fmaf(f, st[i].y, sum);
+    }
+    sum = wave_sum(sum);
+    red[tid] = sum;
+    __syncthreads();
+    sum = (red[0] + red[64]) + (red[128] + red[192]);
+    __syncthreads();
+    // a thread takes four columns of every G-th part
+    const int cols = a.dh / 4, G = kThreads / cols, g = tid / cols, col = (tid - g * cols) * 4;
+    v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (g < G)
+      for (int s = g; s < a.splits; s += G) {
+        const float f = fs[s];
+        if (f == 0.0f) continue;
+        const v4f x = *reinterpret_cast<const v4f*>(a.part + s * a.part_stride + row * a.dh + col);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, x[e], o[e]);
+      }
+    *reinterpret_cast<v4f*>(red + 4 * tid) = o;
+    __syncthreads();
+    const bool any = sum != 0.0f;      // (NaN: some)
+    if (g == 0) {
+      for (int k = 1; k < G; ++k) {
+        const v4f x = *reinterpret_cast<const v4f*>(red + 4 * (tid + k * cols));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += x[e];
+      }
+      const float f = any ? (a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)a.keys_of(b))) / sum : 0.0f;
+      const v4h h = {to_half(o[0] * f), to_half(o[1] * f), to_half(o[2] * f), to_half(o[3] * f)};
+      wt_store(reinterpret_cast<v4h*>(a.out + b * a.out_batch + head * a.out_head + (long)q * a.out_row + col), h);
+    }
+    if (a.lse && tid == 0) a.lse[row] = any ? (m + __builtin_amdgcn_logf(sum)) * kLn2F : -__builtin_inff();
+    return;
+  }
+  const long block = blockIdx.x - joins, group = block / segments;
+  const int seg = (int)(block - group * segments), b = (int)(group / a.kv), kvh = (int)(group % a.kv);
+  const int n = a.keys_of(b), pos = seg * kThreads + tid;
+  if (seg * kThreads >= n) return;
+  float *ms = red, *inv = red + 64, w = 0.0f;
   for (int r0 = 0; r0 < a.rep; r0 += 64) {
     __syncthreads();
-    const int r = r0 + (int)threadIdx.x;
-    if (threadIdx.x < 64 && r < a.rep) {
-      const long row = (long)b * a.heads + kvh * a.rep + r;
+    const int r = r0 + tid;
+    if (tid < 64 && r < a.rep) {
+      const float2* st = a.stats + (long)b * a.heads + kvh * a.rep + r;
       float m = -__builtin_inff(), sum = 0.0f;
-      for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, a.stats[s * stride + row].x);
+      for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, st[s * stride].x);
       for (int s = 0; s < a.splits; ++s) {
-        const float2 st = a.stats[s * stride + row];
-        if (st.y != 0.0f) sum = __builtin_fmaf(__builtin_amdgcn_exp2f(st.x - m), st.y, sum);
+        const float2 x = st[s * stride];
+        if (x.y != 0.0f) sum = __builtin_fmaf(__builtin_amdgcn_exp2f(x.x - m), x.y, sum);
       }
-      ms[threadIdx.x] = m;
-      inv[threadIdx.x] = 1.0f / sum;
+      ms[tid] = m;
+      inv[tid] = 1.0f / sum;
     }
     __syncthreads();
     if (pos < n) {
       const float* s = pg.scores + ((long)b * a.heads + kvh * a.rep + r0) * pg.score_ld + pos;
       const int most = a.rep - r0 < 64 ? a.rep - r0 : 64;
+#pragma unroll 4
       for (int i = 0; i < most; ++i) w = __builtin_fmaf(__builtin_amdgcn_exp2f(s[i * pg.score_ld] - ms[i]), inv[i], w);
     }
   }
@@ -266,7 +400,8 @@ hipError_t with_kernel(long dh, F f) {
   auto go = [&](auto nb) {
     constexpr int NB = decltype(nb)::value;
     static FuncConfig config;
-    constexpr int lds = kWaves * kStep * RowTile<NB>::P;
+    constexpr int lds = kWaves * 2 * kStep * ValueTile<NB, FP8>::P;
+    static_assert(lds >= kWaves * 16 * 32 * NB * 4, "the waves' sums fit");
     if (const hipError_t e = config.ensure((const void*)few_rows_kernel<NB, FP8, PAGED>, lds); e != hipSuccess) return e;
     return f(few_rows_kernel<NB, FP8, PAGED>, lds);
   };
@@ -281,17 +416,34 @@ hipError_t with_kernel(long dh, F f) {
 long ceil_div(long a, long b) { return (a + b - 1) / b; }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// Parts of the positions: workgroups for the device, and no part below one round of the four waves.
+// Parts of the positions: workgroups for the device, and no part below one round of the four waves.  Three per CU, which is how many of a cache of codes run at
+// once (us with 2, 3, 4, 6, 8, 12 per CU: four sequences of 131072 codes 196, 190, 223, 191, 198, 196; 48 of up to 4096 in FP16, where two run, 104, 92, 92, 91, 90, 93).
+constexpr long kPerCu = 3;
 struct Parts {
   int splits, per;
 };
 Parts parts_of(long groups, long most) {
-  const long want = 4l * device_info().cus, rounds = ceil_div(most, kWaves * kStep);
+  const long want = kPerCu * device_info().cus, rounds = ceil_div(most, kWaves * kStep);
   long splits = groups >= want || groups < 1 ? 1 : want / groups;
   if (splits > rounds) splits = rounds;
+  if (splits > kMostParts) splits = kMostParts;
   if (splits < 1) splits = 1;
   const long per = ceil_div(rounds, splits) * kWaves * kStep;
   return {(int)(most > 0 ? ceil_div(most, per) : 1), (int)per};
+}
+
+void divisors(const AttendArgs& a, Pages& pg) {
+  pg.groups = (uint32_t)((long)a.batch * a.kv * a.tiles);
+  pg.by_groups = FastDiv::by(pg.groups);
+  pg.by_tiles = FastDiv::by((uint32_t)a.tiles);
+  pg.by_kv = FastDiv::by((uint32_t)a.kv);
+  pg.by_rep = FastDiv::by((uint32_t)a.rep);
+}
+// weighted: positions that get weights
+hipError_t finish(const AttendArgs& a, const Pages& pg, long weighted, hipStream_t st) {
+  const long joins = a.splits > 1 ? (long)a.batch * a.heads * a.sq : 0, segments = ceil_div(weighted, kThreads), blocks = joins + (long)a.batch * a.kv * segments;
+  if (blocks > 0) finish_kernel<<<(unsigned)blocks, kThreads, 0, st>>>(a, pg, joins, (int)segments);
+  return hipGetLastError();
 }
 
 struct Room {
@@ -344,20 +496,14 @@ hipError_t launch_paged(const PagedCall& c, void* workspace, hipStream_t st) {
   Pages pg{(const uint8_t*)c.cache.k, (const uint8_t*)c.cache.v, c.cache.table, (float*)c.weights, c.weights ? (float*)(ws + r.stats + r.part) : nullptr,
            (c.max_len + 31) / 32 * 32, c.cache.table_ld, c.cache.pages, c.cache.shift};
   const long blocks = c.batch * c.kv_heads * a.tiles * a.splits;
+  divisors(a, pg);
   auto go = [&](auto kernel, int lds) {
     kernel<<<(unsigned)blocks, kThreads, lds, st>>>(a, pg);
     return hipGetLastError();
   };
-  hipError_t e = c.cache.fp8 ? with_kernel<true, true>(c.dh, go) : with_kernel<false, true>(c.dh, go);
+  const hipError_t e = c.cache.fp8 ? with_kernel<true, true>(c.dh, go) : with_kernel<false, true>(c.dh, go);
   if (e != hipSuccess) return e;
-  if (a.splits > 1)
-    if (e = launch_join(a, st); e != hipSuccess) return e;
-  if (c.weights && c.max_len > 0) {
-    const long segments = ceil_div(c.max_len, kThreads);
-    weights_kernel<<<(unsigned)(c.batch * c.kv_heads * segments), kThreads, 0, st>>>(a, pg, (int)segments);
-    e = hipGetLastError();
-  }
-  return e;
+  return finish(a, pg, c.weights ? c.max_len : 0, st);
 }
 
 bool few_rows_take(long heads, long kv_heads, long sq) { return sq * (heads / kv_heads) <= 16; }
@@ -376,11 +522,13 @@ hipError_t launch_few_rows(AttendArgs a, void* workspace, hipStream_t st) {
   a.splits = r.p.splits;
   a.per_split = r.p.per;
   const long blocks = (long)a.batch * a.kv * a.splits;
+  Pages pg{};
+  divisors(a, pg);
   const hipError_t e = with_kernel<false, false>(a.dh, [&](auto kernel, int lds) {
-    kernel<<<(unsigned)blocks, kThreads, lds, st>>>(a, Pages{});
+    kernel<<<(unsigned)blocks, kThreads, lds, st>>>(a, pg);
     return hipGetLastError();
   });
-  return e != hipSuccess || a.splits == 1 ? e : launch_join(a, st);
+  return e != hipSuccess || a.splits == 1 ? e : finish(a, Pages{}, 0, st);
 }
 
 }  // namespace us

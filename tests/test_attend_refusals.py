@@ -61,10 +61,10 @@ CACHE = [dict(batch=-1), dict(batch=65536), dict(kv=0), dict(dh=8), dict(dh=40),
          dict(pages=1 << 31), dict(ld=-1)]
 CASES += [(lambda k=k: f(**k), SHAPE) for k in CACHE for f in (store, paged, evict)]
 CASES += [(lambda d=d: f(dt=d), DTYPE) for d in (us.F32, us.E5M2, 9) for f in (store, paged, evict)]
-CASES += [(lambda: store(s=-1), SHAPE), (lambda: store(layout=L(160, 160, 24)), SHAPE), (lambda: store(layout=L(160, 161, 32)), SHAPE), (lambda: paged(heads=3), SHAPE),
+CASES += [(lambda: store(s=-1), SHAPE), (lambda: store(s=1 << 28), SHAPE), (lambda: store(layout=L(160, 160, 24)), SHAPE), (lambda: store(layout=L(160, 161, 32)), SHAPE), (lambda: paged(heads=3), SHAPE),
           (lambda: paged(heads=0), SHAPE), (lambda: paged(max_len=-1), SHAPE), (lambda: paged(max_len=1 << 31), SHAPE), (lambda: paged(ldq=120), SHAPE), (lambda: paged(ldq=132), SHAPE),
           (lambda: paged(ldo=64), SHAPE), (lambda: paged(ldo=129), SHAPE), (lambda: evict(keep=-1), SHAPE), (lambda: evict(recent=-1), SHAPE), (lambda: evict(recent=21), SHAPE),
-          (lambda: evict(max_len=-1), SHAPE), (lambda: evict(ld_to=2), SHAPE), (lambda: evict(to=32, ld_to=-1), SHAPE)]
+          (lambda: evict(max_len=-1), SHAPE), (lambda: evict(keep=(1 << 20) + 1), SHAPE), (lambda: evict(ld_to=2), SHAPE), (lambda: evict(to=32, ld_to=-1), SHAPE)]
 CASES += [(lambda n=n: store(**{n: None}), NULL) for n in ("K", "V", "kc", "vc", "table", "len")] + [(lambda n=n: store(**{n: 24}), ALIGN) for n in ("K", "V", "kc", "vc")]
 CASES += [(lambda n=n: store(**{n: 18}), ALIGN) for n in ("table", "len", "count")]
 CASES += [(lambda n=n: paged(**{n: None}), NULL) for n in ("Q", "kc", "vc", "table", "len", "O")] + [(lambda n=n: paged(**{n: 24}), ALIGN) for n in ("Q", "kc", "vc", "O", "ws")]
