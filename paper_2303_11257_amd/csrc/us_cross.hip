@@ -32,18 +32,23 @@ struct FwdCfg {
   static constexpr int TILE = BK * RowTile<NB>::P, LDS = 4 * TILE;
 };
 
+// Fragments of rows that are on their way from LDS to the matrix core.
+template <int NB>
+constexpr int kAhead = NB == 1 ? 2 : 4;
+
+// A row's maximum follows its scores only when they outgrow it by 2^kSlack: probabilities are then up to 2^kSlack in between, which FP16 and FP32 hold as exactly,
+// and the sums are hardly ever multiplied again.
+constexpr float kSlack = 8.0f;
+
 template <int NB>
 __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_fwd_kernel(AttendArgs a) {
   using C = FwdCfg<NB>;
-  using T = RowTile<NB>;
   constexpr int BK = C::BK, KB = BK / 32;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  long group, item;
-  group_item(blockIdx.x, (long)a.batch * a.kv, (long)a.rep * a.tiles * a.splits, a.xcds, group, item);
-  const int b = (int)(group / a.kv), kvh = (int)(group % a.kv);
-  const int tile = (int)(item % a.tiles), split = (int)(item / a.tiles % a.splits), head = kvh * a.rep + (int)(item / a.tiles / a.splits);
+  const Items::Item it = a.items.at(blockIdx.x);
+  const int b = it.b, kvh = it.kvh, tile = it.x, split = it.y, head = kvh * a.rep + it.z;
   const int n = a.keys_of(b);
   const int begin = split * a.per_split, end = begin + a.per_split < n ? begin + a.per_split : n;
   const int q = tile * kRows + wave * 32 + l32;
@@ -61,61 +66,105 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_fwd_kernel(At
   if (begin < end) request(begin, 0);
   v8h qf[2 * NB];
   load_fragments<NB>(qf, (const _Float16*)((const uint8_t*)(a.q.p + b * a.q.batch + head * a.q.head) + (long)q * a.q.row), on, a.dh, half);
+  TileReads<NB> at;
+  at.init(lane);
 
   v16f acc[NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) acc[j] = zero16();
   float m = -__builtin_inff(), sum = 0.0f;      // largest raw score, this lane's part of the sum
-  for (int key = begin, i = 0; key < end; key += BK, ++i) {
-    wait_all();
-    __builtin_amdgcn_s_barrier();               // tile i has landed for everyone, tile i - 1 is used up
-    if (key + BK < end) request(key + BK, (i + 1) & 1);
-    const uint8_t *kt = lds + (i & 1) * 2 * C::TILE, *vt = kt + C::TILE;
-    v16f s[KB];
+  const float slack = kSlack / a.c2;
+  constexpr int N = KB * 2 * NB, AHEAD = kAhead<NB>;
+  // raw scores of a tile of keys; each fragment is read while its predecessors are multiplied
+  auto scores = [&](const uint8_t* kt, v16f (&x)[KB]) {
+    // (the blocks of 32 keys in turn: a product that adds to the one just before it has to wait for it)
+    v8h kf[AHEAD];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      s[kb] = zero16();
+    for (int i = 0; i < AHEAD; ++i) kf[i] = at.rows(kt, i % KB, i / KB);
 #pragma unroll
-      for (int t = 0; t < 2 * NB; ++t) s[kb] = mfma32(T::row_fragment(kt, kb, t, l32, half), qf[t], s[kb]);
+    for (int kb = 0; kb < KB; ++kb) x[kb] = zero16();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i % KB] = mfma32(kf[i % AHEAD], qf[i / KB], x[i % KB]);
+      if (i + AHEAD < N) kf[i % AHEAD] = at.rows(kt, (i + AHEAD) % KB, (i + AHEAD) / KB);
     }
+  };
+  // ... made part of the running statistics
+  auto follow = [&](v16f (&x)[KB], int key) {
     if (key + BK > end) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (key + kb * 32 + 8 * (r / 4) + 4 * half + r % 4 >= end) s[kb][r] = -__builtin_inff();
+          if (key + kb * 32 + 8 * (r / 4) + 4 * half + r % 4 >= end) x[kb][r] = -__builtin_inff();
     }
-    float top = s[0][0];
+    float top = x[0][0];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[kb][r]);
-    top = __builtin_fmaxf(m, halves_max(top));
-    const float f = __builtin_amdgcn_exp2f((m - top) * a.c2), neg = -top * a.c2;
-    const bool moved = top > m;
-    m = top;
+      for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, x[kb][r]);
+    top = halves_max(top);
+    const bool moved = top > m + slack;
     if (__builtin_amdgcn_ballot_w64(moved)) {
+      const float f = moved ? __builtin_amdgcn_exp2f((m - top) * a.c2) : 1.0f;
+      if (moved) m = top;
       sum *= f;
 #pragma unroll
       for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[j][r] *= f;
     }
+  };
+  auto step = [&](auto buffer, int key) {
+    constexpr int B = decltype(buffer)::value;
+    tile_landed();                              // this tile has landed for everyone, the one before it is used up
+    if (key + BK < end) request(key + BK, B ^ 1);
+    const uint8_t *kt = lds + B * 2 * C::TILE, *vt = kt + C::TILE;
+    v16f s[KB];
+    v8h vf[NB], p[2 * KB];
+    __builtin_amdgcn_sched_barrier(0);
+    scores(kt, s);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+    for (int j = 0; j < NB; ++j) vf[j] = at.columns(vt, 0, j);
+    next_lds_reads<AHEAD>();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      next_mfma<1>();
+      next_lds_reads<1>();
+    }
+    if constexpr (2 * NB > AHEAD) next_lds_reads<2 * NB - AHEAD>();
+    __builtin_amdgcn_sched_barrier(0);
+    follow(s, key);
+    const float neg = -m * a.c2;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[kb][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][r], a.c2, neg));
         sum += s[kb][r];
       }
+      p[2 * kb] = round8(s[kb], 0);
+      p[2 * kb + 1] = round8(s[kb], 1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+    for (int t = 0; t < 2 * KB; ++t)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const v8h p = round8(s[kb], t);
-#pragma unroll
-        for (int j = 0; j < NB; ++j) acc[j] = mfma32(T::column_fragment(vt, 2 * kb + t, j, lane), p, acc[j]);
+      for (int j = 0; j < NB; ++j) {
+        acc[j] = mfma32(vf[j], p[t], acc[j]);
+        if (t + 1 < 2 * KB) vf[j] = at.columns(vt, t + 1, j);
       }
+#pragma unroll
+    for (int t = 0; t < (2 * KB - 1) * NB; ++t) {
+      next_mfma<1>();
+      next_lds_reads<2>();
+    }
+    next_mfma<NB>();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  for (int key = begin; key < end; key += 2 * BK) {
+    step(std::integral_constant<int, 0>{}, key);
+    if (key + BK < end) step(std::integral_constant<int, 1>{}, key + BK);
   }
   sum = halves_sum(sum);
   const long row = ((long)b * a.heads + head) * a.sq + q;
@@ -130,9 +179,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_fwd_kernel(At
   }
   const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
   const float f = n > 0 ? alpha / sum : 0.0f;
-  _Float16* out = a.out + b * a.out_batch + head * a.out_head + (long)q * a.out_row;
-#pragma unroll
-  for (int j = 0; j < NB; ++j) store_block(out, 32 * j, a.dh, on, half, acc[j], f);
+  store_rows<NB>(lds, acc, f, a.out + b * a.out_batch + head * a.out_head, a.out_row, tile * kRows + wave * 32, a.sq, a.dh, 0, lane, wave);
   if (a.lse && on && half == 0) a.lse[row] = n > 0 ? __builtin_fmaf(__builtin_amdgcn_logf(sum), kLn2F, m * a.c2 * kLn2F) : -__builtin_inff();
 }
 
@@ -168,140 +215,21 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows)
   if (a.lse && lane == 0) a.lse[row] = any ? (m + __builtin_amdgcn_logf(sum)) * kLn2F : -__builtin_inff();
 }
 
-// ---- backward: what the rows need -----------------------------------------------------------------------------------------
-// {log2(e) L - log2(a), D} of every query row, {inf, 0} of the rows that fill the last tile: their P is zero.  16 lanes a row.
-__global__ void __launch_bounds__(kThreads) cross_rows_kernel(AttendArgs a, const float* lse, float2* rows, long total) {
-  const int part = threadIdx.x & 15;
-  const long i = (long)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
-  if (i >= total) return;
-  const long bh = i / a.sqp;
-  const int q = (int)(i - bh * a.sqp), b = (int)(bh / a.heads), head = (int)(bh - (long)b * a.heads);
-  float dot = 0.0f;
-  const int n = a.keys_of(b);
-  const bool on = q < a.sq && n > 0;
-  if (on) {
-    const _Float16* o = (const _Float16*)((const uint8_t*)(a.o.p + b * a.o.batch + head * a.o.head) + (long)q * a.o.row);
-    const _Float16* g = (const _Float16*)((const uint8_t*)(a.g.p + b * a.g.batch + head * a.g.head) + (long)q * a.g.row);
-    for (int c = part * 8; c < a.dh; c += 128) {
-      const v8h x = *reinterpret_cast<const v8h*>(o + c), y = *reinterpret_cast<const v8h*>(g + c);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)x[e], (float)y[e], dot);
-    }
-  }
-  dot = group_sum<16>(dot);
-  if (part == 0) {
-    const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
-    rows[i] = on ? make_float2(__builtin_fmaf(lse[bh * a.sq + q], kLog2eF, -__builtin_amdgcn_logf(alpha)), dot / alpha) : make_float2(__builtin_inff(), 0.0f);
-  }
-}
-
-// ---- backward: dK and dV ------------------------------------------------------------------------------------------------------
-// Heads above 128 columns are accumulated in two halves by two workgroups, whose products with all columns are made twice: 512 registers hold no more.
+// ---- backward: dQ ---------------------------------------------------------------------------------------------------------
+// Comes first and leaves {log2(e) L - log2(a), D} of every query row for dK and dV, {inf, 0} of the rows that fill the last tile: their P is zero.
 template <int NB>
-struct DkvCfg {
-  static constexpr int HALVES = NB > 4 ? 2 : 1, ACC = NB / HALVES;
+struct DqCfg {
+  static constexpr int BK = NB <= 4 ? 64 : 32, TILE = BK * RowTile<NB>::P, LDS = 4 * TILE;
 };
 template <int NB>
-__global__ void __launch_bounds__(kThreads, 1) cross_dkv_kernel(AttendArgs a) {
-  using T = RowTile<NB>;
-  constexpr int BQ = 32, TILE = BQ * T::P, HALVES = DkvCfg<NB>::HALVES, ACC = DkvCfg<NB>::ACC;
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  long group, item;
-  group_item(blockIdx.x, (long)a.batch * a.kv, (long)HALVES * a.tiles * a.splits, a.xcds, group, item);
-  const int b = (int)(group / a.kv), kvh = (int)(group % a.kv), first = (int)(item % HALVES) * ACC;
-  const int tile = (int)(item / HALVES % a.tiles), split = (int)(item / HALVES / a.tiles);
-  const int n = a.keys_of(b);
-  const int key = tile * kRows + wave * 32 + l32;
-  const bool on = key < a.sk, live = key < n;
-  // the tiles of the sharing heads' queries, one head after the other; a split takes per_split of them
-  const int qtiles = (a.sq + BQ - 1) / BQ, total = a.rep * qtiles;
-  const int begin = split * a.per_split;
-  int end = begin + a.per_split < total ? begin + a.per_split : total;
-  if (tile * kRows >= n) end = begin;
-
-  TileLoads<NB, BQ, kThreads> lq, lg;
-  lq.init(a.q.row, a.dh);
-  lg.init(a.g.row, a.dh);
-  auto request = [&](int i, int buffer) {
-    const int head = kvh * a.rep + i / qtiles, q0 = i % qtiles * BQ;
-    uint8_t* to = lds + buffer * 2 * TILE;
-    lq.request((const uint8_t*)(a.q.p + b * a.q.batch + head * a.q.head) + (long)q0 * a.q.row, a.sq - q0, a.q.row, a.dh, to, wave);
-    lg.request((const uint8_t*)(a.g.p + b * a.g.batch + head * a.g.head) + (long)q0 * a.g.row, a.sq - q0, a.g.row, a.dh, to + TILE, wave);
-  };
-  if (begin < end) request(begin, 0);
-  v8h kf[2 * NB], vf[2 * NB];
-  load_fragments<NB>(kf, (const _Float16*)((const uint8_t*)(a.k.p + b * a.k.batch + kvh * a.k.head) + (long)key * a.k.row), live, a.dh, half);
-  load_fragments<NB>(vf, (const _Float16*)((const uint8_t*)(a.v.p + b * a.v.batch + kvh * a.v.head) + (long)key * a.v.row), live, a.dh, half);
-  v16f dk[ACC], dv[ACC];
-#pragma unroll
-  for (int j = 0; j < ACC; ++j) dk[j] = dv[j] = zero16();
-
-  for (int i = begin; i < end; ++i) {
-    wait_all();
-    __builtin_amdgcn_s_barrier();
-    if (i + 1 < end) request(i + 1, (i + 1 - begin) & 1);
-    const uint8_t *qt = lds + ((i - begin) & 1) * 2 * TILE, *gt = qt + TILE;
-    const int head = kvh * a.rep + i / qtiles, q0 = i % qtiles * BQ;
-    const float2* rows = a.rows + ((long)b * a.heads + head) * a.sqp + q0 + 4 * half;
-    v16f s = zero16(), dp = zero16();
-#pragma unroll
-    for (int t = 0; t < 2 * NB; ++t) s = mfma32(T::row_fragment(qt, 0, t, l32, half), kf[t], s);
-#pragma unroll
-    for (int t = 0; t < 2 * NB; ++t) dp = mfma32(T::row_fragment(gt, 0, t, l32, half), vf[t], dp);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float2 ld = rows[8 * (r / 4) + r % 4];
-      s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c2, -ld.x));
-      dp[r] = s[r] * (dp[r] - ld.y);
-    }
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const v8h p = round8(s, t), ds = round8(dp, t);
-#pragma unroll
-      for (int j = 0; j < ACC; ++j) {
-        dv[j] = mfma32(T::column_fragment(gt, t, first + j, lane), p, dv[j]);
-        dk[j] = mfma32(T::column_fragment(qt, t, first + j, lane), ds, dk[j]);
-      }
-    }
-  }
-  const float c = a.c2 * kLn2F;
-#pragma unroll
-  for (int j = 0; j < ACC; ++j) {
-    if (!live) dk[j] = dv[j] = zero16();
-    if (n == 1) dk[j] = zero16();       // the softmax of one key has no gradient
-  }
-  if (a.splits > 1) {
-    float* out = a.part + split * a.part_stride + (((long)b * a.kv + kvh) * a.sk + key) * 2 * a.dh;
-#pragma unroll
-    for (int j = 0; j < ACC; ++j) {
-      store_block_f32(out, 32 * (first + j), a.dh, on, half, dk[j], c);
-      store_block_f32(out + a.dh, 32 * (first + j), a.dh, on, half, dv[j], 1.0f);
-    }
-    return;
-  }
-  const long at = b * a.k.batch + kvh * a.k.head;
-  _Float16 *pk = (_Float16*)((uint8_t*)(a.dk + at) + (long)key * a.k.row), *pv = (_Float16*)((uint8_t*)(a.dv + at) + (long)key * a.k.row);
-#pragma unroll
-  for (int j = 0; j < ACC; ++j) {
-    store_block(pk, 32 * (first + j), a.dh, on, half, dk[j], c * a.beta);
-    store_block(pv, 32 * (first + j), a.dh, on, half, dv[j], a.beta);
-  }
-}
-
-// ---- backward: dQ ---------------------------------------------------------------------------------------------------------
-template <int NB>
 __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(AttendArgs a) {
-  using T = RowTile<NB>;
-  constexpr int BK = 32, TILE = BK * T::P;
+  using C = DqCfg<NB>;
+  constexpr int BK = C::BK, KB = BK / 32, TILE = C::TILE;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  long group, item;
-  group_item(blockIdx.x, (long)a.batch * a.kv, (long)a.rep * a.tiles * a.splits, a.xcds, group, item);
-  const int b = (int)(group / a.kv), kvh = (int)(group % a.kv);
-  const int tile = (int)(item % a.tiles), split = (int)(item / a.tiles % a.splits), head = kvh * a.rep + (int)(item / a.tiles / a.splits);
+  const Items::Item it = a.items.at(blockIdx.x);
+  const int b = it.b, kvh = it.kvh, tile = it.x, split = it.y, head = kvh * a.rep + it.z;
   const int n = a.keys_of(b);
   const int begin = split * a.per_split, end = begin + a.per_split < n ? begin + a.per_split : n;
   const int q = tile * kRows + wave * 32 + l32;
@@ -319,35 +247,91 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
   v8h qf[2 * NB], gf[2 * NB];
   load_fragments<NB>(qf, (const _Float16*)((const uint8_t*)(a.q.p + b * a.q.batch + head * a.q.head) + (long)q * a.q.row), on, a.dh, half);
   load_fragments<NB>(gf, (const _Float16*)((const uint8_t*)(a.g.p + b * a.g.batch + head * a.g.head) + (long)q * a.g.row), on, a.dh, half);
-  const long row = ((long)b * a.heads + head);
+  const long row = (long)b * a.heads + head;
   float2 ld = make_float2(__builtin_inff(), 0.0f);
-  if (on) ld = a.rows[row * a.sqp + q];
+  {
+    float dot = 0.0f;
+    const _Float16* o = (const _Float16*)((const uint8_t*)(a.o.p + b * a.o.batch + head * a.o.head) + (long)q * a.o.row);
+#pragma unroll
+    for (int t = 0; t < 2 * NB; ++t) {
+      const int col = 16 * t + 8 * half;
+      if (on && col < a.dh) {
+        const v8h x = *reinterpret_cast<const v8h*>(o + col);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)x[e], (float)gf[t][e], dot);
+      }
+    }
+    dot = halves_sum(dot);
+    if (on && n > 0) {
+      const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
+      ld = make_float2(__builtin_fmaf(a.lse[row * a.sq + q], kLog2eF, -__builtin_amdgcn_logf(alpha)), dot / alpha);
+    }
+    if (split == 0 && half == 0 && q < a.sqp) a.rows[row * a.sqp + q] = ld;
+  }
+  TileReads<NB> at;
+  at.init(lane);
   v16f acc[NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) acc[j] = zero16();
-  for (int key = begin, i = 0; key < end; key += BK, ++i) {
-    wait_all();
-    __builtin_amdgcn_s_barrier();
-    if (key + BK < end) request(key + BK, (i + 1) & 1);
-    const uint8_t *kt = lds + (i & 1) * 2 * TILE, *vt = kt + TILE;
-    v16f s = zero16(), dp = zero16();
+  constexpr int AHEAD = kAhead<NB>;
+  auto step = [&](auto buffer, int key) {
+    constexpr int B = decltype(buffer)::value;
+    tile_landed();
+    if (key + BK < end) request(key + BK, B ^ 1);
+    const uint8_t *kt = lds + B * 2 * TILE, *vt = kt + TILE;
 #pragma unroll
-    for (int t = 0; t < 2 * NB; ++t) s = mfma32(T::row_fragment(kt, 0, t, l32, half), qf[t], s);
+    for (int kb = 0; kb < KB; ++kb) {
+      // (scores and dO v in turn: a product that adds to the one just before it has to wait for it)
+      auto fragment = [&](int i) { return i % 2 ? at.rows(vt, kb, i / 2) : at.rows(kt, kb, i / 2); };
+      v8h rf[AHEAD], cf[NB];
+      v16f s = zero16(), dp = zero16();
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int t = 0; t < 2 * NB; ++t) dp = mfma32(T::row_fragment(vt, 0, t, l32, half), gf[t], dp);
-    if (key + BK > end) {
+      for (int i = 0; i < AHEAD; ++i) rf[i] = fragment(i);
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (key + 8 * (r / 4) + 4 * half + r % 4 >= end) s[r] = -__builtin_inff();
+      for (int i = 0; i < 4 * NB; ++i) {
+        if (i % 2) dp = mfma32(rf[i % AHEAD], gf[i / 2], dp);
+        else s = mfma32(rf[i % AHEAD], qf[i / 2], s);
+        if (i + AHEAD < 4 * NB) rf[i % AHEAD] = fragment(i + AHEAD);
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j) cf[j] = at.columns(kt, 2 * kb, j);
+      next_lds_reads<AHEAD>();
+#pragma unroll
+      for (int t = 0; t < 4 * NB; ++t) {
+        next_mfma<1>();
+        next_lds_reads<1>();
+      }
+      if constexpr (2 * NB > AHEAD) next_lds_reads<2 * NB - AHEAD>();
+      __builtin_amdgcn_sched_barrier(0);
+      if (key + BK > end) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (key + kb * 32 + 8 * (r / 4) + 4 * half + r % 4 >= end) s[r] = -__builtin_inff();
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c2, -ld.x)) * (dp[r] - ld.y);
+      const v8h ds[2] = {round8(dp, 0), round8(dp, 1)};
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          acc[j] = mfma32(cf[j], ds[t], acc[j]);
+          if (t == 0) cf[j] = at.columns(kt, 2 * kb + 1, j);
+        }
+#pragma unroll
+      for (int t = 0; t < NB; ++t) {
+        next_mfma<1>();
+        next_lds_reads<2>();
+      }
+      next_mfma<NB>();
+      __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dp[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c2, -ld.x)) * (dp[r] - ld.y);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const v8h ds = round8(dp, t);
-#pragma unroll
-      for (int j = 0; j < NB; ++j) acc[j] = mfma32(T::column_fragment(kt, t, j, lane), ds, acc[j]);
-    }
+  };
+  for (int key = begin; key < end; key += 2 * BK) {
+    step(std::integral_constant<int, 0>{}, key);
+    if (key + BK < end) step(std::integral_constant<int, 1>{}, key + BK);
   }
   const float c = a.c2 * kLn2F;
   if (n == 1) {
@@ -360,9 +344,169 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
     for (int j = 0; j < NB; ++j) store_block_f32(out, 32 * j, a.dh, on, half, acc[j], c);
     return;
   }
-  _Float16* out = a.out + b * a.out_batch + head * a.out_head + (long)q * a.out_row;
+  store_rows<NB>(lds, acc, c * a.beta, a.out + b * a.out_batch + head * a.out_head, a.out_row, tile * kRows + wave * 32, a.sq, a.dh, 0, lane, wave);
+}
+
+// ---- backward: dK and dV ------------------------------------------------------------------------------------------------------
+// A wave takes 32 keys, whose fragments and gradients stay in registers, and all queries of the heads that share them, tile by tile through LDS.
+// Heads above 128 columns are accumulated in two halves by two workgroups, whose products with all columns are made twice: 512 registers hold no more.
+template <int NB>
+struct DkvCfg {
+  static constexpr int HALVES = NB > 4 ? 2 : 1, ACC = NB / HALVES;
+  static constexpr int BQ = NB <= 4 ? 64 : 32, TILE = BQ * RowTile<NB>::P, STATS = 1024, STAGE = 2 * TILE + STATS, LDS = 3 * STAGE;
+};
+// Scores and dO v of 32 queries and a wave's keys.
+struct DkvBlock {
+  v16f s, dp;
+};
+template <int NB>
+__global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(AttendArgs a) {
+  using C = DkvCfg<NB>;
+  constexpr int BQ = C::BQ, QB = BQ / 32, TILE = C::TILE, ACC = C::ACC, AHEAD = kAhead<NB>;
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Items::Item it = a.items.at(blockIdx.x);
+  const int b = it.b, kvh = it.kvh, tile = it.y, split = it.z, first = it.x * ACC;
+  const int n = a.keys_of(b);
+  const int key = tile * kRows + wave * 32 + l32;
+  const bool on = key < a.sk;
+  // the tiles of the sharing heads' queries, one head after the other; a split takes per_split of them
+  const int qtiles = (a.sq + BQ - 1) / BQ, total = a.rep * qtiles;
+  const int begin = split * a.per_split;
+  int end = begin + a.per_split < total ? begin + a.per_split : total;
+  if (tile * kRows >= n) end = begin;
+
+  TileLoads<NB, BQ, kThreads> lq, lg;
+  lq.init(a.q.row, a.dh);
+  lg.init(a.g.row, a.dh);
+  int rhead = begin / (qtiles > 0 ? qtiles : 1), rtile = begin - rhead * qtiles;      // of the next request
+  auto request = [&](int buffer) {
+    const int head = kvh * a.rep + rhead, q0 = rtile * BQ;
+    uint8_t* to = lds + buffer * C::STAGE;
+    lq.request((const uint8_t*)(a.q.p + b * a.q.batch + head * a.q.head) + (long)q0 * a.q.row, a.sq - q0, a.q.row, a.dh, to, wave);
+    lg.request((const uint8_t*)(a.g.p + b * a.g.batch + head * a.g.head) + (long)q0 * a.g.row, a.sq - q0, a.g.row, a.dh, to + TILE, wave);
+    if (wave == 0) load_to_lds(buffer_words(a.rows + ((long)b * a.heads + head) * a.sqp + q0, BQ * 8), to + 2 * TILE, (uint32_t)lane * 16);
+    if (++rtile == qtiles) { rtile = 0; ++rhead; }
+  };
+  if (begin < end) request(0);
+  v8h kf[2 * NB], vf[2 * NB];
+  load_fragments<NB>(kf, (const _Float16*)((const uint8_t*)(a.k.p + b * a.k.batch + kvh * a.k.head) + (long)key * a.k.row), key < n, a.dh, half);
+  load_fragments<NB>(vf, (const _Float16*)((const uint8_t*)(a.v.p + b * a.v.batch + kvh * a.v.head) + (long)key * a.v.row), key < n, a.dh, half);
+  TileReads<NB, ACC> at;
+  at.init(lane, first);
+  v16f dk[ACC], dv[ACC];
 #pragma unroll
-  for (int j = 0; j < NB; ++j) store_block(out, 32 * j, a.dh, on, half, acc[j], c * a.beta);
+  for (int j = 0; j < ACC; ++j) dk[j] = dv[j] = zero16();
+
+  auto products = [&](const uint8_t* qt, int qb, DkvBlock& x) {
+    // (scores and dO v in turn: a product that adds to the one just before it has to wait for it)
+    auto fragment = [&](int i) { return at.rows(i % 2 ? qt + TILE : qt, qb, i / 2); };
+    v8h rf[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) rf[i] = fragment(i);
+    x.s = x.dp = zero16();
+#pragma unroll
+    for (int i = 0; i < 4 * NB; ++i) {
+      if (i % 2) x.dp = mfma32(rf[i % AHEAD], vf[i / 2], x.dp);
+      else x.s = mfma32(rf[i % AHEAD], kf[i / 2], x.s);
+      if (i + AHEAD < 4 * NB) rf[i % AHEAD] = fragment(i + AHEAD);
+    }
+  };
+  // Block qb of the tile at qt becomes part of the gradients; meanwhile block nqb of the tile at nt is made, so that matrix core and vector ALU both have work.
+  auto block = [&](DkvBlock& cur, const uint8_t* qt, int qb, DkvBlock& next, const uint8_t* nt, int nqb) {
+    const uint8_t *gt = qt + TILE, *st = gt + TILE;
+    v4f ld[4][2];
+    v8h p[2], ds[2], gc[ACC], qc[ACC];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) ld[r][e] = *US_LDS_AT(const v4f, st + (qb * 32 + 8 * r + 4 * half) * 8 + 16 * e);
+    products(nt, nqb, next);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const v4f x = ld[r / 4][r % 4 / 2];
+      cur.s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(cur.s[r], a.c2, -x[r % 2 * 2]));
+      cur.dp[r] = cur.s[r] * (cur.dp[r] - x[r % 2 * 2 + 1]);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      p[t] = round8(cur.s, t);
+      ds[t] = round8(cur.dp, t);
+    }
+#pragma unroll
+    for (int j = 0; j < ACC; ++j) gc[j] = at.columns(gt, 2 * qb, j);
+    next_lds_reads<8 + AHEAD>();
+#pragma unroll
+    for (int i = 0; i < 4 * NB; ++i) {
+      next_mfma<1>();
+      next_lds_reads<1>();
+      next_exp<(16 + 4 * NB - 1) / (4 * NB)>();
+      next_valu<(64 + 4 * NB - 1) / (4 * NB)>();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int j = 0; j < ACC; ++j) {
+        dv[j] = mfma32(gc[j], p[t], dv[j]);
+        qc[j] = at.columns(qt, 2 * qb + t, j);
+      }
+#pragma unroll
+      for (int j = 0; j < ACC; ++j) {
+        dk[j] = mfma32(qc[j], ds[t], dk[j]);
+        if (t == 0) gc[j] = at.columns(gt, 2 * qb + 1, j);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 3 * ACC; ++t) {
+      next_mfma<1>();
+      next_lds_reads<2>();
+    }
+    next_mfma<ACC>();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // A tile's last block is needed while the next tile's first one is made, and the tile behind that is on its way: three buffers.  Behind the last tile a block is
+  // made of what the next buffer happens to hold, and not used: a branch around it would have the accumulators moved about at its end.
+  DkvBlock x, y;
+  if (begin < end) {
+    tile_landed();
+    if (begin + 1 < end) request(1);
+    products(lds, 0, x);
+    for (int i = begin, buffer = 0; i < end; ++i) {
+      const int after = buffer == 2 ? 0 : buffer + 1;
+      const uint8_t *qt = lds + buffer * C::STAGE, *nt = lds + after * C::STAGE;
+      if constexpr (QB > 1) block(x, qt, 0, y, qt, 1);
+      tile_landed();                            // the next tile has landed for everyone, the one before this is used up
+      if (i + 2 < end) request(after == 2 ? 0 : after + 1);
+      if constexpr (QB > 1) {
+        block(y, qt, 1, x, nt, 0);
+      } else {
+        block(x, qt, 0, y, nt, 0);
+        x = y;
+      }
+      buffer = after;
+    }
+  }
+  const float c = a.c2 * kLn2F;
+#pragma unroll
+  for (int j = 0; j < ACC; ++j) {
+    if (key >= n) dk[j] = dv[j] = zero16();
+    if (n == 1) dk[j] = zero16();       // the softmax of one key has no gradient
+  }
+  if (a.splits > 1) {
+    float* out = a.part + split * a.part_stride + (((long)b * a.kv + kvh) * a.sk + key) * 2 * a.dh;
+#pragma unroll
+    for (int j = 0; j < ACC; ++j) {
+      store_block_f32(out, 32 * (first + j), a.dh, on, half, dk[j], c);
+      store_block_f32(out + a.dh, 32 * (first + j), a.dh, on, half, dv[j], 1.0f);
+    }
+    return;
+  }
+  const long at_head = b * a.k.batch + kvh * a.k.head;
+  store_rows<ACC>(lds, dk, c * a.beta, a.dk + at_head, a.k.row / 2, tile * kRows + wave * 32, a.sk, a.dh, 32 * first, lane, wave);
+  store_rows<ACC>(lds, dv, a.beta, a.dv + at_head, a.k.row / 2, tile * kRows + wave * 32, a.sk, a.dh, 32 * first, lane, wave);
 }
 
 // Sums of split gradients, part after part: `rows` rows of dh columns `row_stride` elements apart in a part; row = (batch * heads + head) * s + t.
@@ -387,7 +531,7 @@ __global__ void __launch_bounds__(kThreads) cross_sum_kernel(const float* part, 
 
 // f(integral_constant<int, NB>): blocks of 32 columns that hold a head
 template <class F>
-hipError_t with_blocks(long dh, F f) {
+auto with_blocks(long dh, F f) {
   if (dh <= 32) return f(std::integral_constant<int, 1>{});
   if (dh <= 64) return f(std::integral_constant<int, 2>{});
   if (dh <= 96) return f(std::integral_constant<int, 3>{});
@@ -395,6 +539,9 @@ hipError_t with_blocks(long dh, F f) {
   if (dh <= 192) return f(std::integral_constant<int, 6>{});
   return f(std::integral_constant<int, 8>{});
 }
+
+// (rows of a tile of queries)
+long padded_rows(long sq) { return (sq + 63) / 64 * 64; }
 
 Side side(const void* p, const us_heads_layout& l) { return Side{(const _Float16*)p, l.batch, l.head, (int)(2 * l.row)}; }
 
@@ -411,10 +558,9 @@ AttendArgs cross_args(const CrossCall& c) {
   a.kv = (int)c.kv_heads;
   a.rep = (int)(c.heads / c.kv_heads);
   a.sq = (int)c.sq;
-  a.sqp = (int)((c.sq + 31) / 32 * 32);
+  a.sqp = (int)padded_rows(c.sq);
   a.sk = (int)c.sk;
   a.dh = (int)c.dh;
-  a.xcds = device_info().xcds;
   a.c2 = (float)(1.0 / sqrt((double)c.dh) * 1.44269504088896340736);
   a.alpha = c.alpha;
   return a;
@@ -436,11 +582,16 @@ Cut cut(long items, long steps, long least) {
   return {steps > 0 ? (int)ceil_div(steps, per) : 1, per};
 }
 Cut fwd_cut(const CrossCall& c) { return cut(c.batch * c.heads * ceil_div(c.sq, kRows), ceil_div(c.sk, 64), 4); }
-Cut dq_cut(const CrossCall& c) { return cut(c.batch * c.heads * ceil_div(c.sq, kRows), ceil_div(c.sk, 32), 8); }
-Cut dkv_cut(const CrossCall& c) { return cut(c.batch * c.kv_heads * ceil_div(c.sk, kRows), c.heads / c.kv_heads * ceil_div(c.sq, 32), 8); }
+Cut dq_cut(const CrossCall& c) { return cut(c.batch * c.heads * ceil_div(c.sq, kRows), ceil_div(c.sk, 64), 4); }
+Cut dkv_cut(const CrossCall& c) {
+  return with_blocks(c.dh, [&](auto nb) {
+    using C = DkvCfg<decltype(nb)::value>;
+    return cut(C::HALVES * c.batch * c.kv_heads * ceil_div(c.sk, kRows), c.heads / c.kv_heads * ceil_div(c.sq, C::BQ), 256 / C::BQ);
+  });
+}
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-size_t rows_bytes(const CrossCall& c) { return up256((size_t)c.batch * c.heads * ((c.sq + 31) / 32 * 32) * 8); }
+size_t rows_bytes(const CrossCall& c) { return up256((size_t)c.batch * c.heads * padded_rows(c.sq) * 8); }
 
 template <class K>
 hipError_t launch(K kernel, FuncConfig& config, long blocks, int lds, const AttendArgs& a, hipStream_t st) {
@@ -490,6 +641,7 @@ hipError_t launch_cross_fwd(const CrossCall& c, void* workspace, hipStream_t st)
   const hipError_t e = with_blocks(c.dh, [&](auto nb) {
     constexpr int NB = decltype(nb)::value;
     static FuncConfig config;
+    a.items = Items::of(c.batch * c.kv_heads, c.kv_heads, a.tiles, a.splits, a.rep, device_info().xcds);
     return launch(cross_fwd_kernel<NB>, config, c.batch * c.heads * a.tiles * a.splits, FwdCfg<NB>::LDS, a, st);
   });
   if (e != hipSuccess || a.splits == 1) return e;
@@ -497,60 +649,58 @@ hipError_t launch_cross_fwd(const CrossCall& c, void* workspace, hipStream_t st)
 }
 
 hipError_t launch_cross_bwd(const CrossCall& c, void* dQ, void* dK, void* dV, float beta_q, float beta_kv, void* workspace, hipStream_t st) {
+  const int xcds = device_info().xcds;
   AttendArgs a = cross_args(c);
-  float2* row_values = (float2*)workspace;
-  a.rows = row_values;
+  a.rows = (float2*)workspace;
   a.part = (float*)((uint8_t*)workspace + rows_bytes(c));
-  const long total = c.batch * c.heads * a.sqp;
-  hipError_t e = hipSuccess;
-  if (total > 0) {
-    cross_rows_kernel<<<(unsigned)ceil_div(total, kThreads / 16), kThreads, 0, st>>>(a, c.lse, row_values, total);
-    if (e = hipGetLastError(); e != hipSuccess) return e;
+  a.lse = c.lse;
+  if (c.sq > 0) {
+    AttendArgs q = a;
+    q.out = (_Float16*)dQ;
+    q.out_batch = c.lq.batch;
+    q.out_head = c.lq.head;
+    q.out_row = c.lq.row;
+    q.beta = beta_q;
+    q.tiles = (int)ceil_div(c.sq, kRows);
+    const Cut s = dq_cut(c);
+    q.splits = s.splits;
+    q.per_split = (int)(s.per * 64);
+    q.part_stride = c.batch * c.heads * c.sq * c.dh;
+    q.items = Items::of(c.batch * c.kv_heads, c.kv_heads, q.tiles, q.splits, q.rep, xcds);
+    hipError_t e = with_blocks(c.dh, [&](auto nb) {
+      constexpr int NB = decltype(nb)::value;
+      static FuncConfig config;
+      return launch(cross_dq_kernel<NB>, config, c.batch * c.heads * q.tiles * q.splits, DqCfg<NB>::LDS, q, st);
+    });
+    if (e != hipSuccess) return e;
+    if (q.splits > 1) {
+      const long rows = c.batch * c.heads * c.sq;
+      cross_sum_kernel<<<(unsigned)ceil_div(rows * (c.dh / 4), kThreads), kThreads, 0, st>>>(q.part, q.part_stride, c.dh, q.splits, rows, (int)c.heads, (int)c.sq, (int)c.dh, q.out,
+                                                                                            q.out_batch, q.out_head, q.out_row, beta_q);
+      if (e = hipGetLastError(); e != hipSuccess) return e;
+    }
   }
-
-  AttendArgs k = a;
-  k.dk = (_Float16*)dK;
-  k.dv = (_Float16*)dV;
-  k.beta = beta_kv;
-  k.tiles = (int)ceil_div(c.sk, kRows);
-  const Cut ks = dkv_cut(c);
-  k.splits = ks.splits;
-  k.per_split = (int)ks.per;
-  k.part_stride = c.batch * c.kv_heads * c.sk * c.dh * 2;
-  if (c.sk > 0) e = with_blocks(c.dh, [&](auto nb) {
+  if (c.sk == 0) return hipSuccess;
+  a.dk = (_Float16*)dK;
+  a.dv = (_Float16*)dV;
+  a.beta = beta_kv;
+  const Cut s = dkv_cut(c);
+  a.splits = s.splits;
+  a.per_split = (int)s.per;
+  a.part_stride = c.batch * c.kv_heads * c.sk * c.dh * 2;
+  hipError_t e = with_blocks(c.dh, [&](auto nb) {
     constexpr int NB = decltype(nb)::value;
+    using C = DkvCfg<NB>;
     static FuncConfig config;
-    return launch(cross_dkv_kernel<NB>, config, DkvCfg<NB>::HALVES * c.batch * c.kv_heads * k.tiles * k.splits, 4 * 32 * RowTile<NB>::P, k, st);
-  });
-  if (e != hipSuccess) return e;
-  if (k.splits > 1) {
-    const long rows = c.batch * c.kv_heads * c.sk;
-    for (int i = 0; i < 2; ++i)
-      cross_sum_kernel<<<(unsigned)ceil_div(rows * (c.dh / 4), kThreads), kThreads, 0, st>>>(k.part + i * c.dh, k.part_stride, 2 * c.dh, k.splits, rows, (int)c.kv_heads,
-                                                                                            (int)c.sk, (int)c.dh, i ? k.dv : k.dk, c.lkv.batch, c.lkv.head, c.lkv.row, beta_kv);
-    if (e = hipGetLastError(); e != hipSuccess) return e;
-  }
-
-  if (c.sq == 0) return e;
-  a.out = (_Float16*)dQ;
-  a.out_batch = c.lq.batch;
-  a.out_head = c.lq.head;
-  a.out_row = c.lq.row;
-  a.beta = beta_q;
-  a.tiles = (int)ceil_div(c.sq, kRows);
-  const Cut qs = dq_cut(c);
-  a.splits = qs.splits;
-  a.per_split = (int)(qs.per * 32);
-  a.part_stride = c.batch * c.heads * c.sq * c.dh;
-  e = with_blocks(c.dh, [&](auto nb) {
-    constexpr int NB = decltype(nb)::value;
-    static FuncConfig config;
-    return launch(cross_dq_kernel<NB>, config, c.batch * c.heads * a.tiles * a.splits, 4 * 32 * RowTile<NB>::P, a, st);
+    a.tiles = (int)ceil_div(c.sk, kRows);
+    a.items = Items::of(c.batch * c.kv_heads, c.kv_heads, C::HALVES, a.tiles, a.splits, xcds);
+    return launch(cross_dkv_kernel<NB>, config, C::HALVES * c.batch * c.kv_heads * a.tiles * a.splits, C::LDS, a, st);
   });
   if (e != hipSuccess || a.splits == 1) return e;
-  const long rows = c.batch * c.heads * c.sq;
-  cross_sum_kernel<<<(unsigned)ceil_div(rows * (c.dh / 4), kThreads), kThreads, 0, st>>>(a.part, a.part_stride, c.dh, a.splits, rows, (int)c.heads, (int)c.sq, (int)c.dh, a.out,
-                                                                                        a.out_batch, a.out_head, a.out_row, beta_q);
+  const long rows = c.batch * c.kv_heads * c.sk;
+  for (int i = 0; i < 2; ++i)
+    cross_sum_kernel<<<(unsigned)ceil_div(rows * (c.dh / 4), kThreads), kThreads, 0, st>>>(a.part + i * c.dh, a.part_stride, 2 * c.dh, a.splits, rows, (int)c.kv_heads, (int)c.sk,
+                                                                                          (int)c.dh, i ? a.dv : a.dk, c.lkv.batch, c.lkv.head, c.lkv.row, beta_kv);
   return hipGetLastError();
 }
 

@@ -37,31 +37,48 @@ struct RowTile {
     if (P == 128) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
     return ((row & 3) << 2) | ((row >> 2) & 3);
   }
-  // rows as the first operand of the 32 x 32 x 16 instruction: lane l has row l % 32 (+ 32 rb), columns 16 t + 8 (l / 32) ..
-  __device__ __forceinline__ static v8h row_fragment(const uint8_t* tile, int rb, int t, int l32, int half) {
-    const int row = rb * 32 + l32;
-    return *US_LDS_AT(const v8h, tile + row * P + (((2 * t + half) ^ swz(row)) << 4));
+};
+
+// Where a lane reads its parts of a tile, in bytes from the tile's start.
+// (COLS: blocks of columns that it takes transposed, from block `first` on)
+template <int NB, int COLS = NB>
+struct TileReads {
+  using T = RowTile<NB>;
+  uint32_t row[2 * NB], col[2][COLS];
+  __device__ __forceinline__ void init(int lane, int first = 0) {
+    const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
+#pragma unroll
+    for (int t = 0; t < 2 * NB; ++t) row[t] = (uint32_t)(l32 * T::P + (((2 * t + half) ^ T::swz(l32)) << 4));
+    // (a bit of the swizzle changes from a row to the row 8 further on)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) {
+        const int r = 4 * half + (l16 >> 2) + 8 * e, chunk = (first + j) * 4 + ((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1);
+        col[e][j] = (uint32_t)(r * T::P + ((chunk ^ T::swz(r)) << 4) + (l16 & 1) * 8);
+      }
   }
-  // ... and transposed: lane l has column 32 nb + l % 32 and the rows 16 t + 4 (l / 32) + (0 .. 3, 8 .. 11), which are the rows that the
+  // rows as the first operand of the 32 x 32 x 16 instruction: lane l has row 32 rb + l % 32, columns 16 t + 8 (l / 32) ..
+  __device__ __forceinline__ v8h rows(const uint8_t* tile, int rb, int t) const { return *US_LDS_AT(const v8h, tile + row[t] + rb * 32 * T::P); }
+  // ... and transposed: lane l has column 32 j + l % 32 and the rows 16 t + 4 (l / 32) + (0 .. 3, 8 .. 11), which are the rows that the
   // results of a 32 x 32 instruction leave in a lane
-  __device__ __forceinline__ static v8h column_fragment(const uint8_t* tile, int t, int nb, int lane) {
-    const int l16 = lane & 15, row = 16 * t + 4 * (lane >> 5) + (l16 >> 2);
-    const int chunk = nb * 4 + ((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1);
-    // (the rows 8 further on: swz() changes by a bit that the four rows share)
-    const uint8_t* at = tile + row * P + ((chunk ^ swz(row)) << 4) + (l16 & 1) * 8;
-    const uint8_t* at8 = tile + (row + 8) * P + ((chunk ^ swz(row + 8)) << 4) + (l16 & 1) * 8;
-    const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(US_LDS_AT(v4s, at));
-    const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(US_LDS_AT(v4s, at8));
+  __device__ __forceinline__ v8h columns(const uint8_t* tile, int t, int j) const {
+    const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(US_LDS_AT(v4s, tile + col[0][j] + t * 16 * T::P));
+    const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(US_LDS_AT(v4s, tile + col[1][j] + t * 16 * T::P));
     struct { v4s a, b; } both = {a, b};
     return __builtin_bit_cast(v8h, both);
   }
 };
 
-// 16 bytes per lane straight to LDS, lane after lane from `lds` on; zeros where the offset lies beyond the resource.  (A function of its own: from inside a lambda
-// that a kernel template calls, the compiler's host pass leaves out the kernel's stub.)
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t* lds, int off) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, US_LDS_AT(void, lds), 16, off, 0, 0, 0);
+// 16 bytes per lane straight to LDS, lane after lane from `lds` on; zeros where the offset lies beyond the resource (its four words: buffer_words).  In assembly,
+// because the compiler makes transposing reads of LDS wait for every such load that it knows of, the next tile's too: the kernels wait for what they need themselves
+// (tile_landed, wait_newest).  The compiler's own waits count fewer loads than there are, and so wait longer, never shorter.  (s_nop: five wait states between a
+// vector instruction that writes a scalar register and this load's reading it, one between m0 and the load.)
+__device__ __forceinline__ void load_to_lds(v4i from, uint8_t* lds, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)US_LDS_AT(uint8_t, lds)), "v"(off), "s"(from) : "memory");
 }
+// All loads of the workgroup to LDS have landed, all its reads of LDS are done; nothing that reads or writes memory moves across.
+__device__ __forceinline__ void tile_landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // The loads of a tile of ROWS rows by THREADS threads, straight to LDS; rows from `rows` on and columns from dh on are zeros.
 template <int NB, int ROWS, int THREADS>
@@ -78,16 +95,13 @@ struct TileLoads {
   }
   __device__ __forceinline__ void request(const void* base, long rows, int row_bytes, int dh, uint8_t* lds, int wave) const {
     const int r = rows > ROWS ? ROWS : rows < 0 ? 0 : (int)rows;
-    const __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, r > 0 ? (r - 1) * row_bytes + dh * 2 : 0, 0x00027000);
+    const v4i res = buffer_words(base, r > 0 ? (uint32_t)((r - 1) * row_bytes + dh * 2) : 0u);
 #pragma unroll
     for (int j = 0; j < LD; ++j)
       if (BYTES / 16 % THREADS == 0 || j * THREADS + wave * 64 < BYTES / 16)
-        load_to_lds(res, lds + (j * THREADS + wave * 64) * 16, (int)off[j]);
+        load_to_lds(res, lds + (j * THREADS + wave * 64) * 16, off[j]);
   }
 };
-
-// all of the wave's loads have landed and its LDS reads are done
-__device__ __forceinline__ void wait_all() { __builtin_amdgcn_s_waitcnt(0x0070); }
 
 __device__ __forceinline__ v16f zero16() {
   v16f z;
@@ -105,26 +119,46 @@ __device__ __forceinline__ v8h round8(const v16f& x, int t) {
   return h;
 }
 
-// A lane's 32 x 32 block of results, column l % 32 of the block being a row of memory: rows 8 q + 4 (l / 32) .. + 3 are four of that row's columns;
-// the two halves of the wave exchange quads, so that each lane stores 16 bytes: columns 16 k + 8 (l / 32) .. + 7, k = 0, 1.
-__device__ __forceinline__ void store_block(_Float16* row, int col0, int dh, bool on, int half, const v16f& x, float f) {
+// Eight of a lane's sixteen results of a 32 x 32 block, rounded: the block's column l % 32 is a row of memory, a lane has the columns 8 q + 4 (l / 32) .. + 3 of
+// that row; the two halves of the wave exchange quads, so that each lane gets the columns 16 k + 8 (l / 32) .. + 7.
+__device__ __forceinline__ v4i eight_columns(const v16f& x, int k, float f) {
+  v4i o;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    v2i lo, hi;
+  for (int e = 0; e < 2; ++e) {
+    const v2h a = {to_half(x[8 * k + 2 * e] * f), to_half(x[8 * k + 2 * e + 1] * f)};
+    const v2h b = {to_half(x[8 * k + 4 + 2 * e] * f), to_half(x[8 * k + 5 + 2 * e] * f)};
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned p = r[0], q = r[1];
+    o[e] = (int)p;
+    o[2 + e] = (int)q;
+  }
+  return o;
+}
+// A wave's 32 rows of COLS blocks of 32 columns (from column `col0` on) to memory, through LDS: whole rows at a time.  From the registers a store would write 32 bytes
+// of each row, and memory takes such pieces at a fraction of its rate (16 x 16 heads of 64, 512 queries over up to 1024 keys: dK and dV 92 -> 73 us, O 41 -> 34).  Every wave of the workgroup calls it; rows from `rows` on and columns from dh on
+// stay as they are.
+template <int COLS>
+__device__ __forceinline__ void store_rows(uint8_t* lds, const v16f (&x)[COLS], float f, _Float16* base, long row_stride, int row0, int rows, int dh, int col0, int lane,
+                                           int wave) {
+  constexpr int G = COLS <= 4 ? COLS : COLS / 2, PITCH = 64 * G + 16;      // blocks at a time
+  uint8_t* mine = lds + wave * 32 * PITCH;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const v2h a = {to_half(x[8 * k + 2 * e] * f), to_half(x[8 * k + 2 * e + 1] * f)};
-      const v2h b = {to_half(x[8 * k + 4 + 2 * e] * f), to_half(x[8 * k + 5 + 2 * e] * f)};
-      const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
-      const unsigned p = r[0], q = r[1];
-      lo[e] = (int)p;
-      hi[e] = (int)q;
+  for (int g = 0; g < COLS; g += G) {
+    __syncthreads();                 // the tiles, or the blocks before these, are used up
+#pragma unroll
+    for (int j = 0; j < G; ++j)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) *US_LDS_AT(v4i, mine + (lane & 31) * PITCH + (4 * j + 2 * k + (lane >> 5)) * 16) = eight_columns(x[g + j], k, f);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 2 * G; ++i) {
+      const int c = i * 64 + lane, row = c / (4 * G), chunk = c - row * (4 * G), col = col0 + 32 * g + 8 * chunk;
+      const v4i o = *US_LDS_AT(const v4i, mine + row * PITCH + chunk * 16);
+      if (row0 + row < rows && col < dh) wt_store(reinterpret_cast<v4i*>(base + (row0 + row) * row_stride + col), o);
     }
-    const int col = col0 + 16 * k + 8 * half;
-    if (on && col < dh) wt_store(reinterpret_cast<v4i*>(row + col), v4i{lo[0], lo[1], hi[0], hi[1]});
   }
 }
-// ... and in FP32
+// Such a block in FP32, 16 bytes a lane.
 __device__ __forceinline__ void store_block_f32(float* row, int col0, int dh, bool on, int half, const v16f& x, float f) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
@@ -133,17 +167,47 @@ __device__ __forceinline__ void store_block_f32(float* row, int col0, int dh, bo
   }
 }
 
-// Work item of a workgroup whose groups (of `per` items that read the same keys) go to one XCD each, where there are enough of them.
-__device__ __forceinline__ void group_item(long block, long groups, long per, int xcds, long& group, long& item) {
-  if (xcds > 1 && groups % xcds == 0) {
-    const long xcd = block % xcds, i = block / xcds;
-    group = i / per * xcds + xcd;
-    item = i % per;
-  } else {
-    group = block / per;
-    item = block % per;
+// What a workgroup does: item `x` of `nx`, `y` of `ny`, `z` of `nz` of a group that reads the same keys, all of them on one XCD where the groups can be dealt out
+// evenly.  The host prepares the divisions.
+struct Items {
+  FastDiv by_xcds, by_per, by_x, by_y, by_kv;
+  uint32_t xcds, per, nx, ny, kv;
+  static Items of(long groups, long kv, long nx, long ny, long nz, int xcds) {
+    Items i;
+    i.xcds = groups % xcds == 0 ? (uint32_t)xcds : 1u;
+    i.per = (uint32_t)(nx * ny * nz);
+    i.nx = (uint32_t)nx;
+    i.ny = (uint32_t)ny;
+    i.kv = (uint32_t)kv;
+    i.by_xcds = FastDiv::by(i.xcds);
+    i.by_per = FastDiv::by(i.per);
+    i.by_x = FastDiv::by(i.nx);
+    i.by_y = FastDiv::by(i.ny);
+    i.by_kv = FastDiv::by(i.kv);
+    return i;
   }
-}
+  struct Item {
+    int b, kvh, x, y, z;
+  };
+  __device__ __forceinline__ Item at(uint32_t block) const {
+    const uint32_t i = by_xcds.of(block), xcd = block - i * xcds, q = by_per.of(i), group = q * xcds + xcd;
+    uint32_t r = i - q * per;
+    Item it;
+    it.b = (int)by_kv.of(group);
+    it.kvh = (int)(group - (uint32_t)it.b * kv);
+    const uint32_t rx = by_x.of(r), ry = by_y.of(rx);
+    it.x = (int)(r - rx * nx);
+    it.y = (int)(rx - ry * ny);
+    it.z = (int)ry;
+    return it;
+  }
+};
+
+// Scheduling: n instructions of a kind next
+template <int N> __device__ __forceinline__ void next_mfma() { __builtin_amdgcn_sched_group_barrier(0x008, N, 0); }
+template <int N> __device__ __forceinline__ void next_valu() { __builtin_amdgcn_sched_group_barrier(0x002, N, 0); }
+template <int N> __device__ __forceinline__ void next_exp() { __builtin_amdgcn_sched_group_barrier(0x400, N, 0); }
+template <int N> __device__ __forceinline__ void next_lds_reads() { __builtin_amdgcn_sched_group_barrier(0x100, N, 0); }
 
 // What the kernels need of a call.
 struct Side {               // a tensor of heads, strides in elements
@@ -157,11 +221,12 @@ struct AttendArgs {
   _Float16 *out, *dk, *dv;  // O or dQ (out_batch ..), dK and dV (laid out as k)
   long out_batch, out_head, out_row;
   float* lse;               // forward: L, or NULL
-  const float2* rows;       // backward: {log2(e) L - log2(a), D} of [batch * heads][sqp]
+  float2* rows;             // backward: {log2(e) L - log2(a), D} of [batch * heads][sqp]
   float* part;              // parts of split sums
   float2* stats;            // forward: {largest score (base 2), sum} of a part's rows
   long part_stride;         // elements between parts
-  int batch, heads, kv, rep, sq, sqp, sk, dh, tiles, splits, per_split, xcds;
+  Items items;
+  int batch, heads, kv, rep, sq, sqp, sk, dh, tiles, splits, per_split;
   float c2, alpha, beta;    // c2 = dh^-1/2 log2(e);  alpha <= 0: n^1/2;  beta: factor of the gradient's store
   __device__ __forceinline__ int keys_of(int b) const {
     const int n = klen ? klen[b] : sk;

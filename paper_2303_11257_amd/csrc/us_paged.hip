@@ -138,10 +138,9 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
     const long o0 = at0 < 0 ? 0 : at0 * row_bytes, o1 = at1 < 0 ? 0 : at1 * row_bytes;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc((void*)(vbase + (i ? o1 : o0)), 0, i ? bytes1 : bytes0, 0x00027000);
+      const v4i res = buffer_words(vbase + (i ? o1 : o0), (uint32_t)(i ? bytes1 : bytes0));
 #pragma unroll
-      for (int j = 0; j < VL; ++j)
-        load_to_lds(res, vt + i * 16 * T::P + j * 1024, voff[FP8 ? i : 0][j]);
+      for (int j = 0; j < VL; ++j) load_to_lds(res, vt + i * 16 * T::P + j * 1024, (uint32_t)voff[FP8 ? i : 0][j]);
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
