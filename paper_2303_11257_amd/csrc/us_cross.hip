@@ -217,6 +217,10 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows)
 
 // ---- backward: dQ ---------------------------------------------------------------------------------------------------------
 // Comes first and leaves {log2(e) L - log2(a), D} of every query row for dK and dV, {inf, 0} of the rows that fill the last tile: their P is zero.
+// D from the rounded O is off by 2^-12 |O| / a of dO, which next to dO v of n keys is 2^-12 (sum p^2)^1/2: of few keys as much as dS's own rounding.  Up to kFewKeys
+// keys D is therefore the sum of p dO v itself, from products made twice (2-norm error of dQ, unit normal inputs, 5 to 120 keys: 2.95e-4 to 2.98e-4, two roundings to FP16; of 140 to 400 keys, from O,
+// 3.2e-4 to 3.1e-4).
+constexpr int kFewKeys = 128;
 template <int NB>
 struct DqCfg {
   static constexpr int BK = NB <= 4 ? 64 : 32, TILE = BK * RowTile<NB>::P, LDS = 4 * TILE;
@@ -247,9 +251,35 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
   v8h qf[2 * NB], gf[2 * NB];
   load_fragments<NB>(qf, (const _Float16*)((const uint8_t*)(a.q.p + b * a.q.batch + head * a.q.head) + (long)q * a.q.row), on, a.dh, half);
   load_fragments<NB>(gf, (const _Float16*)((const uint8_t*)(a.g.p + b * a.g.batch + head * a.g.head) + (long)q * a.g.row), on, a.dh, half);
+  TileReads<NB> at;
+  at.init(lane);
+  constexpr int AHEAD = kAhead<NB>, CA = NB <= 4 ? NB : 4;
+  // raw scores and dO v of 32 keys, in turn: a product that adds to the one just before it has to wait for it
+  auto products = [&](const uint8_t* kt, int kb, v16f& s, v16f& dp) {
+    auto fragment = [&](int i) { return at.rows(i % 2 ? kt + TILE : kt, kb, i / 2); };
+    v8h rf[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) rf[i] = fragment(i);
+    s = dp = zero16();
+#pragma unroll
+    for (int i = 0; i < 4 * NB; ++i) {
+      if (i % 2) dp = mfma32(rf[i % AHEAD], gf[i / 2], dp);
+      else s = mfma32(rf[i % AHEAD], qf[i / 2], s);
+      if (i + AHEAD < 4 * NB) rf[i % AHEAD] = fragment(i + AHEAD);
+    }
+  };
+  auto mask = [&](v16f& s, int key) {
+    if (key + 32 > end) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (key + 8 * (r / 4) + 4 * half + r % 4 >= end) s[r] = -__builtin_inff();
+    }
+  };
   const long row = (long)b * a.heads + head;
   float2 ld = make_float2(__builtin_inff(), 0.0f);
-  {
+  const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
+  if (on && n > 0) ld.x = __builtin_fmaf(a.lse[row * a.sq + q], kLog2eF, -__builtin_amdgcn_logf(alpha));
+  if (n > kFewKeys) {
     float dot = 0.0f;
     const _Float16* o = (const _Float16*)((const uint8_t*)(a.o.p + b * a.o.batch + head * a.o.head) + (long)q * a.o.row);
 #pragma unroll
@@ -261,71 +291,72 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
         for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)x[e], (float)gf[t][e], dot);
       }
     }
-    dot = halves_sum(dot);
-    if (on && n > 0) {
-      const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
-      ld = make_float2(__builtin_fmaf(a.lse[row * a.sq + q], kLog2eF, -__builtin_amdgcn_logf(alpha)), dot / alpha);
+    if (on) ld.y = halves_sum(dot) / alpha;
+  } else if (begin < end) {
+    float ps = 0.0f, pd = 0.0f;
+    for (int key = begin, buffer = 0; key < end; key += BK, buffer ^= 1) {
+      tile_landed();
+      if (key + BK < end) request(key + BK, buffer ^ 1);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        v16f s, dp;
+        products(lds + buffer * 2 * TILE, kb, s, dp);
+        mask(s, key + 32 * kb);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c2, -ld.x));
+          ps += p;
+          pd = __builtin_fmaf(p, dp[r], pd);
+        }
+      }
     }
-    if (split == 0 && half == 0 && q < a.sqp) a.rows[row * a.sqp + q] = ld;
+    ps = halves_sum(ps);
+    pd = halves_sum(pd);
+    if (on) ld.y = pd / ps;
+    tile_landed();
+    request(begin, 0);
   }
-  TileReads<NB> at;
-  at.init(lane);
+  if (split == 0 && half == 0 && q < a.sqp) a.rows[row * a.sqp + q] = ld;
   v16f acc[NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) acc[j] = zero16();
-  constexpr int AHEAD = kAhead<NB>;
   auto step = [&](auto buffer, int key) {
     constexpr int B = decltype(buffer)::value;
     tile_landed();
     if (key + BK < end) request(key + BK, B ^ 1);
-    const uint8_t *kt = lds + B * 2 * TILE, *vt = kt + TILE;
+    const uint8_t* kt = lds + B * 2 * TILE;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      // (scores and dO v in turn: a product that adds to the one just before it has to wait for it)
-      auto fragment = [&](int i) { return i % 2 ? at.rows(vt, kb, i / 2) : at.rows(kt, kb, i / 2); };
-      v8h rf[AHEAD], cf[NB];
-      v16f s = zero16(), dp = zero16();
+      v8h cf[CA];
+      v16f s, dp;
       __builtin_amdgcn_sched_barrier(0);
+      products(kt, kb, s, dp);
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) rf[i] = fragment(i);
-#pragma unroll
-      for (int i = 0; i < 4 * NB; ++i) {
-        if (i % 2) dp = mfma32(rf[i % AHEAD], gf[i / 2], dp);
-        else s = mfma32(rf[i % AHEAD], qf[i / 2], s);
-        if (i + AHEAD < 4 * NB) rf[i % AHEAD] = fragment(i + AHEAD);
-      }
-#pragma unroll
-      for (int j = 0; j < NB; ++j) cf[j] = at.columns(kt, 2 * kb, j);
+      for (int j = 0; j < CA; ++j) cf[j] = at.columns(kt, 2 * kb, j);
       next_lds_reads<AHEAD>();
 #pragma unroll
       for (int t = 0; t < 4 * NB; ++t) {
         next_mfma<1>();
         next_lds_reads<1>();
       }
-      if constexpr (2 * NB > AHEAD) next_lds_reads<2 * NB - AHEAD>();
+      if constexpr (2 * CA > AHEAD) next_lds_reads<2 * CA - AHEAD>();
       __builtin_amdgcn_sched_barrier(0);
-      if (key + BK > end) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (key + kb * 32 + 8 * (r / 4) + 4 * half + r % 4 >= end) s[r] = -__builtin_inff();
-      }
+      mask(s, key + 32 * kb);
 #pragma unroll
       for (int r = 0; r < 16; ++r) dp[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c2, -ld.x)) * (dp[r] - ld.y);
       const v8h ds[2] = {round8(dp, 0), round8(dp, 1)};
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int i = 0; i < 2 * NB; ++i) {
+        acc[i % NB] = mfma32(cf[i % CA], ds[i / NB], acc[i % NB]);
+        if (i + CA < 2 * NB) cf[i % CA] = at.columns(kt, 2 * kb + (i + CA) / NB, (i + CA) % NB);
+      }
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-          acc[j] = mfma32(cf[j], ds[t], acc[j]);
-          if (t == 0) cf[j] = at.columns(kt, 2 * kb + 1, j);
-        }
-#pragma unroll
-      for (int t = 0; t < NB; ++t) {
+      for (int t = 0; t < 2 * NB - CA; ++t) {
         next_mfma<1>();
         next_lds_reads<2>();
       }
-      next_mfma<NB>();
+      next_mfma<CA>();
       __builtin_amdgcn_sched_barrier(0);
     }
   };
