@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
     }
     const int t = row / a.rep, hd = kvh * a.rep + (row - t * a.rep);
     const long at = ((long)b * a.heads + hd) * a.sq + t;
-    if (col == 0 && (parts || a.stats)) a.stats[split * (a.part_stride / a.dh) + at] = make_float2(top, total);
+    if (col == 0 && a.stats) a.stats[split * (a.part_stride / a.dh) + at] = make_float2(top, total);
     if (col == 0 && !parts && a.lse) a.lse[at] = total > 0.0f || total != total ? (top + __builtin_amdgcn_logf(total)) * kLn2F : -__builtin_inff();
     if (col >= a.dh) continue;
     if (parts) {
@@ -296,6 +296,34 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
       const float f = total == 0.0f ? 0.0f : alpha / total;
       const v4h h = {to_half(o[0] * f), to_half(o[1] * f), to_half(o[2] * f), to_half(o[3] * f)};
       wt_store(reinterpret_cast<v4h*>(a.out + b * a.out_batch + hd * a.out_head + (long)t * a.out_row + col), h);
+    }
+  }
+  if constexpr (PAGED) {
+    // all scores of the key head's rows are this workgroup's: their weights, without another launch
+    if (pg.scores && !a.stats) {
+      __shared__ float ms[16], inv[16];
+      if (threadIdx.x < 16) {
+        const int r = (int)threadIdx.x;
+        float top = wm[0][r], total = 0.0f;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) top = __builtin_fmaxf(top, wm[w][r]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+          if (ws[w][r] != 0.0f) total = __builtin_fmaf(__builtin_amdgcn_exp2f(wm[w][r] - top), ws[w][r], total);
+        ms[r] = top;
+        inv[r] = 1.0f / total;
+      }
+      __threadfence_block();
+      __syncthreads();
+      for (int at = (int)threadIdx.x; at < end; at += kThreads) {
+        const int page = pg.table[(long)b * pg.table_ld + (at >> pg.shift)];
+        if (page < 0 || page >= pg.pages) continue;
+        float* const to = pg.weights + (((long)page * a.kv + kvh) << pg.shift) + (at & ((1 << pg.shift) - 1));
+        const float* s = pg.scores + ((long)b * a.heads + kvh * a.rep) * pg.score_ld + at;
+        float w = *to;
+        for (int r = 0; r < nrows; ++r) w = __builtin_fmaf(__builtin_amdgcn_exp2f(s[r * pg.score_ld] - ms[r]), inv[r], w);
+        *to = w;
+      }
     }
   }
 }
@@ -365,6 +393,13 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(AttendArgs a, Pages pg
   const int seg = (int)(block - group * segments), b = (int)(group / a.kv), kvh = (int)(group % a.kv);
   const int n = a.keys_of(b), pos = seg * kThreads + tid;
   if (seg * kThreads >= n) return;
+  // (everything that can be read at once is: the page, the first rows' scores, the parts' statistics)
+  int page = -1;
+  if (pos < n) page = pg.table[(long)b * pg.table_ld + (pos >> pg.shift)];
+  const float* scores = pg.scores + ((long)b * a.heads + kvh * a.rep) * pg.score_ld + pos;
+  float early[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) early[i] = pos < n && i < a.rep ? scores[i * pg.score_ld] : 0.0f;
   float *ms = red, *inv = red + 64, w = 0.0f;
   for (int r0 = 0; r0 < a.rep; r0 += 64) {
     __syncthreads();
@@ -372,24 +407,34 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(AttendArgs a, Pages pg
     if (tid < 64 && r < a.rep) {
       const float2* st = a.stats + (long)b * a.heads + kvh * a.rep + r;
       float m = -__builtin_inff(), sum = 0.0f;
-      for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, st[s * stride].x);
-      for (int s = 0; s < a.splits; ++s) {
-        const float2 x = st[s * stride];
-        if (x.y != 0.0f) sum = __builtin_fmaf(__builtin_amdgcn_exp2f(x.x - m), x.y, sum);
+      // running, eight parts' statistics in flight
+      for (int s = 0; s < a.splits; s += 8) {
+        float2 x[8];
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          x[k] = s + k < a.splits ? st[(s + k) * stride] : make_float2(-__builtin_inff(), 0.0f);
+          top = __builtin_fmaxf(top, x[k].x);
+        }
+        sum = sum == 0.0f ? 0.0f : sum * __builtin_amdgcn_exp2f(m - top);
+        m = top;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (x[k].y != 0.0f) sum = __builtin_fmaf(__builtin_amdgcn_exp2f(x[k].x - m), x[k].y, sum);
       }
       ms[tid] = m;
       inv[tid] = 1.0f / sum;
     }
     __syncthreads();
     if (pos < n) {
-      const float* s = pg.scores + ((long)b * a.heads + kvh * a.rep + r0) * pg.score_ld + pos;
       const int most = a.rep - r0 < 64 ? a.rep - r0 : 64;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (r0 == 0 && i < most) w = __builtin_fmaf(__builtin_amdgcn_exp2f(early[i] - ms[i]), inv[i], w);
 #pragma unroll 4
-      for (int i = 0; i < most; ++i) w = __builtin_fmaf(__builtin_amdgcn_exp2f(s[i * pg.score_ld] - ms[i]), inv[i], w);
+      for (int i = r0 == 0 ? 4 : 0; i < most; ++i) w = __builtin_fmaf(__builtin_amdgcn_exp2f(scores[(r0 + i) * pg.score_ld] - ms[i]), inv[i], w);
     }
   }
-  if (pos >= n) return;
-  const int page = pg.table[(long)b * pg.table_ld + (pos >> pg.shift)];
   if (page < 0 || page >= pg.pages) return;
   pg.weights[(((long)page * a.kv + kvh) << pg.shift) + (pos & ((1 << pg.shift) - 1))] += w;
 }
@@ -445,6 +490,7 @@ hipError_t finish(const AttendArgs& a, const Pages& pg, long weighted, hipStream
   return hipGetLastError();
 }
 
+constexpr long kOwnWeights = 1024;      // four positions a thread
 struct Room {
   size_t stats, part, scores;      // bytes
   Parts p;
@@ -453,7 +499,8 @@ Room room(long batch, long heads, long kv, long rows_per_kv, long sq, long dh, l
   Room r{};
   r.p = parts_of(batch * kv * ceil_div(rows_per_kv, 16), most);
   const size_t rows = (size_t)batch * heads * sq;
-  if (r.p.splits > 1 || weights) r.stats = up256(r.p.splits * rows * 8);
+  // (one part of all of a key head's rows and not many positions: its workgroup adds the weights itself)
+  if (r.p.splits > 1 || (weights && (rows_per_kv > 16 || most > kOwnWeights))) r.stats = up256(r.p.splits * rows * 8);
   if (r.p.splits > 1) r.part = up256(r.p.splits * rows * dh * 4);
   if (weights) r.scores = rows * ((most + 31) / 32 * 32) * 4;
   return r;
@@ -502,7 +549,7 @@ hipError_t launch_paged(const PagedCall& c, void* workspace, hipStream_t st) {
   };
   const hipError_t e = c.cache.fp8 ? with_kernel<true, true>(c.dh, go) : with_kernel<false, true>(c.dh, go);
   if (e != hipSuccess) return e;
-  return finish(a, pg, c.weights ? c.max_len : 0, st);
+  return finish(a, pg, c.weights && a.stats ? c.max_len : 0, st);
 }
 
 bool few_rows_take(long heads, long kv_heads, long sq) { return sq * (heads / kv_heads) <= 16; }
