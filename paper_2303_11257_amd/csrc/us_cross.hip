@@ -541,23 +541,25 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
 }
 
 // Sums of split gradients, part after part: `rows` rows of dh columns `row_stride` elements apart in a part; row = (batch * heads + head) * s + t.
+// blockIdx.y = 1: the second gradient, dh columns further on.
 __global__ void __launch_bounds__(kThreads) cross_sum_kernel(const float* part, long part_stride, long row_stride, int splits, long rows, int heads, int s, int dh,
-                                                             _Float16* out, long out_batch, long out_head, long out_row, float beta) {
+                                                             _Float16* first, _Float16* second, long out_batch, long out_head, long out_row, float beta) {
   const int per = dh / 4;
   const long i = (long)blockIdx.x * kThreads + threadIdx.x;
   const long row = i / per;
   if (row >= rows) return;
   const int col = (int)(i - row * per) * 4;
-  const float* p = part + row * row_stride + col;
-  v4f sum = *reinterpret_cast<const v4f*>(p);
-  for (int k = 1; k < splits; ++k) {
+  const float* p = part + row * row_stride + col + blockIdx.y * dh;
+  v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int k = 0; k < splits; ++k) {
     const v4f x = *reinterpret_cast<const v4f*>(p + k * part_stride);
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] += x[e];
   }
   const long bh = row / s, t = row - bh * s, b = bh / heads, head = bh - b * heads;
   const v4h o = {to_half(sum[0] * beta), to_half(sum[1] * beta), to_half(sum[2] * beta), to_half(sum[3] * beta)};
-  wt_store(reinterpret_cast<v4h*>(out + b * out_batch + head * out_head + t * out_row + col), o);
+  wt_store(reinterpret_cast<v4h*>((blockIdx.y ? second : first) + b * out_batch + head * out_head + t * out_row + col), o);
 }
 
 // f(integral_constant<int, NB>): blocks of 32 columns that hold a head
@@ -706,7 +708,7 @@ hipError_t launch_cross_bwd(const CrossCall& c, void* dQ, void* dK, void* dV, fl
     if (e != hipSuccess) return e;
     if (q.splits > 1) {
       const long rows = c.batch * c.heads * c.sq;
-      cross_sum_kernel<<<(unsigned)ceil_div(rows * (c.dh / 4), kThreads), kThreads, 0, st>>>(q.part, q.part_stride, c.dh, q.splits, rows, (int)c.heads, (int)c.sq, (int)c.dh, q.out,
+      cross_sum_kernel<<<(unsigned)ceil_div(rows * (c.dh / 4), kThreads), kThreads, 0, st>>>(q.part, q.part_stride, c.dh, q.splits, rows, (int)c.heads, (int)c.sq, (int)c.dh, q.out, nullptr,
                                                                                             q.out_batch, q.out_head, q.out_row, beta_q);
       if (e = hipGetLastError(); e != hipSuccess) return e;
     }
@@ -729,9 +731,8 @@ hipError_t launch_cross_bwd(const CrossCall& c, void* dQ, void* dK, void* dV, fl
   });
   if (e != hipSuccess || a.splits == 1) return e;
   const long rows = c.batch * c.kv_heads * c.sk;
-  for (int i = 0; i < 2; ++i)
-    cross_sum_kernel<<<(unsigned)ceil_div(rows * (c.dh / 4), kThreads), kThreads, 0, st>>>(a.part + i * c.dh, a.part_stride, 2 * c.dh, a.splits, rows, (int)c.kv_heads, (int)c.sk,
-                                                                                          (int)c.dh, i ? a.dv : a.dk, c.lkv.batch, c.lkv.head, c.lkv.row, beta_kv);
+  cross_sum_kernel<<<dim3((unsigned)ceil_div(rows * (c.dh / 4), kThreads), 2), kThreads, 0, st>>>(a.part, a.part_stride, 2 * c.dh, a.splits, rows, (int)c.kv_heads, (int)c.sk,
+                                                                                                 (int)c.dh, a.dk, a.dv, c.lkv.batch, c.lkv.head, c.lkv.row, beta_kv);
   return hipGetLastError();
 }
 

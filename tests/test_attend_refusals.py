@@ -56,7 +56,7 @@ APART = [L(0, 160, 32), L(640, 0, 32), L(640, 64, 32), L(640, 32, 64), L(320, 32
 CASES += [(lambda k=k: fwd(lo=k), SHAPE) for k in APART] + [(lambda k=k: bwd(lq=k), SHAPE) for k in APART] + [(lambda: bwd(lkv=L(0, 224, 32)), SHAPE), (lambda: bwd(lkv=L(448, 0, 32)), SHAPE)]
 CASES += [(lambda n=n: bwd(**{n: None}), NULL) for n in ("Q", "K", "V", "O", "lse", "dO", "dQ", "dK", "dV")]
 CASES += [(lambda n=n: bwd(**{n: 24}), ALIGN) for n in ("Q", "K", "V", "O", "dO", "dQ", "dK", "dV", "ws")] + [(lambda: bwd(klen=17), ALIGN), (lambda: bwd(lse=17), ALIGN)]
-CASES += [(lambda: bwd(ws=None), WORKSPACE), (lambda: bwd(wsb=16), WORKSPACE), (lambda: fwd(batch=1, heads=1, kv=1, sq=100, sk=9000, ws=OK, wsb=64), WORKSPACE)]
+CASES += [(lambda: bwd(sk=200, ws=None), WORKSPACE), (lambda: bwd(sk=200, wsb=16), WORKSPACE), (lambda: fwd(batch=1, heads=1, kv=1, sq=100, sk=9000, ws=OK, wsb=64), WORKSPACE)]
 CACHE = [dict(batch=-1), dict(batch=65536), dict(kv=0), dict(dh=8), dict(dh=40), dict(dh=272), dict(page=8), dict(page=24), dict(page=2048), dict(page=0), dict(pages=-1),
          dict(pages=1 << 31), dict(ld=-1)]
 CASES += [(lambda k=k: f(**k), SHAPE) for k in CACHE for f in (store, paged, evict)]
@@ -92,7 +92,7 @@ def test_nothing_to_do_is_no_error():
 
 def test_sizes():
     assert us.attention_cross_workspace_bytes(0, 4, 2, 5, 7, 32) == 0 and us.attention_cross_workspace_bytes(2, 4, 3, 5, 7, 32) == 0
-    assert us.attention_cross_workspace_bytes(2, 4, 2, 5, 7, 32) >= 2 * 4 * 32 * 8
+    assert us.attention_cross_workspace_bytes(2, 4, 2, 5, 200, 32) >= 2 * 4 * 64 * 8
     assert us.attention_paged_workspace_bytes(0, 4, 2, 32, 100, True) == 0 and us.attention_paged_workspace_bytes(2, 4, 3, 32, 100, True) == 0
     assert us.attention_paged_workspace_bytes(2, 4, 2, 32, 100, True) >= 2 * 4 * 100 * 4
     assert us.attention_cross_workspace_bytes(2, 4, 2, 0, 7, 32) == us.attention_cross_workspace_bytes(2, 4, 2, 0, 0, 32) == 0

@@ -96,6 +96,9 @@ SHAPES = [
     (1, 2, 1, 100, 257, 112), (1, 2, 2, 65, 193, 128), (1, 2, 1, 40, 97, 160), (1, 2, 2, 70, 66, 192), (1, 1, 1, 35, 129, 208), (1, 4, 1, 50, 70, 256),
     # one and a few queries: the rows of a key head's sharing heads together
     (3, 4, 4, 1, 300, 64), (2, 8, 1, 1, 129, 128), (1, 16, 1, 1, 1000, 96), (2, 4, 2, 7, 31, 80), (1, 2, 1, 8, 515, 256), (1, 6, 3, 5, 33, 16), (2, 3, 3, 16, 200, 192),
+    # up to 128 keys and just beyond, every width, many queries over them (sums in parts)
+    (1, 2, 1, 70, 128, 32), (1, 2, 2, 33, 128, 64), (2, 2, 2, 100, 128, 96), (1, 4, 2, 65, 128, 128), (1, 2, 2, 40, 127, 16), (1, 1, 1, 32, 16, 128), (1, 2, 1, 70, 129, 32),
+    (1, 2, 1, 1100, 128, 64), (1, 1, 1, 2000, 77, 128), (2, 2, 1, 700, 5, 80), (1, 1, 1, 64, 128, 144), (2, 3, 3, 2, 100, 112),
     # few queries over many keys, and the other way round: reductions in parts
     (1, 1, 1, 40, 3000, 64), (1, 2, 1, 20, 2500, 128), (1, 1, 1, 2900, 40, 64), (1, 4, 1, 1500, 33, 80), (1, 1, 1, 1, 5001, 32), (1, 1, 1, 30, 1400, 256),
 ]
@@ -110,7 +113,7 @@ def test_forward_and_backward(dims):
 
 
 @pytest.mark.parametrize("klen", [[0, 1, 2, 70], [70, 69, 64, 63], [65, 33, 0, 200], [-5, 1, 1, 1], [0, 0, 0, 0]], ids=str)
-@pytest.mark.parametrize("sq,heads,dh", [(1, 2, 64), (37, 4, 80), (140, 2, 128)])
+@pytest.mark.parametrize("sq,heads,dh", [(1, 2, 64), (37, 4, 80), (140, 2, 128), (37, 2, 160)])
 @pytest.mark.parametrize("fill", [float("nan"), float("inf"), -65504.0])
 def test_lengths_hide_what_lies_behind(klen, sq, heads, dh, fill):
     """Keys and values behind an item's length are NaN, infinite or FP16's lowest; lengths beyond sk are cut to it; no key, one key."""
