@@ -546,9 +546,10 @@ typedef struct {
  * Q, O, dO, dQ: FP16, `heads` heads of sq tokens; K, V, dK, dV: FP16, kv_heads heads of sk tokens; kv_heads divides heads (query head i takes key head
  * i / (heads / kv_heads)); dh a multiple of 16 up to US_ROPE_HEAD_MAX.  lq: layout of Q and dQ, lkv: of K, V, dK and dV, lo: of O and dO (host pointers, each may
  * be NULL).  Keys and values that several batch items share have a batch stride of 0 in the forward call; heads and rows of the tensors that a call
- * writes must not overlap (US_ERR_SHAPE).
+ * writes must not overlap (US_ERR_SHAPE).  batch and heads up to 65535, batch * heads * ceil(sq / 128) and batch * kv_heads * ceil(sk / 128) up to 2^22.
  * Scores, statistics and all sums are FP32; p, alpha p and ds are rounded to FP16 for their second product, as us_attention_* rounds P and dA (values beyond
- * FP16's range become infinities).  O is read in the backward pass for sum p dp = dO O / alpha.
+ * FP16's range become infinities).  O is read in the backward pass of more than 128 keys, for
+ * sum p dp = dO O / alpha.
  * Workspace (16-byte aligned, contents undefined on entry and exit): us_attention_cross_workspace_bytes, asked with the device current that runs the calls,
  * serves both.  The forward call can do without (NULL: few queries over many keys are then slower, and are added in another order); the backward call needs it.
  * Calls that may overlap on a GPU need a workspace each.  Outputs must not overlap inputs or one another.
@@ -587,7 +588,8 @@ size_t us_attention_cross_workspace_bytes(long batch, long heads, long kv_heads,
  *   new_len[b] = min(len[b], keep) (int32 [batch], may be len itself, or NULL), kept: int32 [batch, kv_heads, keep], the positions that were kept, -1 behind a shorter
  *   sequence's.  0 <= recent <= keep <= 2^20.  max_len as above.
  *
- * dh a multiple of 16 up to US_ROPE_HEAD_MAX; batch and heads up to 65535.  All pools and rows 16-byte aligned.  Results do not depend on scheduling.
+ * dh a multiple of 16 up to US_ROPE_HEAD_MAX; batch and heads up to 65535; batch * heads up to 2^22, batch * kv_heads * ceil(max_len / 256) up to 2^23 (eviction:
+ * batch * kv_heads up to 2^20); a sequence's new rows, s * kv_heads * dh / 8, up to 2^31 - 1.  All pools and rows 16-byte aligned.  Results do not depend on scheduling.
  */
 #define US_CACHE_PAGE_MAX 1024
 us_status us_cache_store(const void* K, const void* V, const us_heads_layout* l, void* k_cache, void* v_cache, us_dtype cache_dt, long pages, long page,

@@ -927,8 +927,9 @@ static us_status cross_shape(long batch, long heads, long kv_heads, long sq, lon
   constexpr long kMost = 1L << 28;
   if (batch < 0 || batch > 65535 || heads < 1 || heads > 65535 || kv_heads < 1 || heads % kv_heads != 0 || sq < 0 || sq > kMost || sk < 0 || sk > kMost) return US_ERR_SHAPE;
   if (dh < 16 || dh > US_ROPE_HEAD_MAX || !mult16(dh)) return US_ERR_SHAPE;
-  // (workgroups are counted in 31 bits)
-  if (batch * heads * ((sq + 127) / 128) > (1L << 30) || batch * kv_heads * ((sk + 127) / 128) > (1L << 30)) return US_ERR_SHAPE;
+  // (a launch has fewer than 2^32 threads, and the rows of a key head are counted in 31 bits)
+  constexpr long kTiles = 1L << 22;
+  if (batch * heads * ((sq + 127) / 128) > kTiles || batch * kv_heads * ((sk + 127) / 128) > kTiles) return US_ERR_SHAPE;
   return US_OK;
 }
 
@@ -1008,8 +1009,8 @@ us_status us_cache_store(const void* K, const void* V, const us_heads_layout* l,
 
 static us_status paged_shape(long batch, long heads, long kv_heads, long dh, long max_len) {
   if (heads < 1 || heads > 65535 || heads % kv_heads != 0 || max_len < 0 || max_len > (1L << 30)) return US_ERR_SHAPE;
-  // (workgroups are counted in 31 bits)
-  if (batch * heads > (1L << 28) || batch * kv_heads * ((max_len + 255) / 256) > (1L << 30)) return US_ERR_SHAPE;
+  // (a launch has fewer than 2^32 threads)
+  if (batch * heads > (1L << 22) || batch * kv_heads * ((max_len + 255) / 256) > (1L << 23)) return US_ERR_SHAPE;
   return US_OK;
 }
 
@@ -1046,8 +1047,8 @@ us_status us_cache_evict(void* k_cache, void* v_cache, float* weights, us_dtype 
   if (us_status e = cache_shape(cache_dt, pages, page, table_ld, batch, kv_heads, dh); e != US_OK) return e;
   if (max_len < 0 || max_len > (1L << 30) || keep < 0 || keep > (1L << 30) || recent < 0 || recent > keep || table_to_ld < 0 || table_to_ld > (1L << 28)) return US_ERR_SHAPE;
   if (table_to == table && table_to_ld != table_ld) return US_ERR_SHAPE;
-  // (workgroups are counted in 31 bits, parts of a sequence in 16)
-  if (batch * kv_heads > (1L << 28) || keep > (1L << 20)) return US_ERR_SHAPE;
+  // (a launch has fewer than 2^32 threads, and parts of a sequence are counted in 16 bits)
+  if (batch * kv_heads > (1L << 20) || keep > (1L << 20)) return US_ERR_SHAPE;
   if (batch == 0) return US_OK;
   if (!len || (keep > 0 && (!k_cache || !v_cache || !weights || !table || !table_to || !kept))) return US_ERR_NULL;
   if (!aligned16(k_cache) || !aligned16(v_cache) || ((uintptr_t)weights & 3) || ((uintptr_t)table & 3) || ((uintptr_t)table_to & 3) || ((uintptr_t)len & 3) ||

@@ -25,16 +25,62 @@ __device__ __forceinline__ void load_fragments(v8h (&f)[2 * NB], const _Float16*
   }
 }
 
+// Row r of a key head: query q of its h-th head.  `again`: worked out anew, so that no register holds it through the loop over the keys (the forward kernel of 64
+// columns, 512 x 1024: 130 registers a lane and three waves a SIMD 38 us, 128 and four 34).
+struct RowAt {
+  int h, q, head;
+  __device__ __forceinline__ RowAt(const AttendArgs& a, int kvh, int r, bool again = false) {
+    if (again) asm volatile("" : "+v"(r));
+    h = (int)a.by_sq.of((uint32_t)r);
+    q = r - h * a.sq;
+    head = kvh * a.rep + h;
+  }
+  __device__ __forceinline__ long of_all(const AttendArgs& a, int b) const { return ((long)b * a.heads + head) * a.sq + q; }
+};
+// Where the rows of a key head's O or dQ start, and those of dK or dV.  (No reference to the kernel's arguments: those are then no longer scalars.)
+struct RowsOfHeads {
+  FastDiv by_sq;
+  _Float16* base;
+  long head, row;
+  int sq, rows;
+  __device__ __forceinline__ RowsOfHeads(const AttendArgs& a, int b, int kvh, int nrows)
+      : by_sq(a.by_sq), base(a.out + b * a.out_batch + kvh * a.rep * a.out_head), head(a.out_head), row(a.out_row), sq(a.sq), rows(nrows) {}
+  __device__ __forceinline__ _Float16* operator()(int r) const {
+    if (r >= rows) return nullptr;
+    const int h = (int)by_sq.of((uint32_t)r);
+    return base + h * head + (r - h * sq) * row;
+  }
+};
+struct RowsOf {
+  uint8_t* base;
+  int row_bytes, rows;
+  __device__ __forceinline__ _Float16* operator()(int r) const { return r < rows ? (_Float16*)(base + (long)r * row_bytes) : nullptr; }
+};
+
 // ---- forward -----------------------------------------------------------------------------------------------------------
 template <int NB>
 struct FwdCfg {
-  static constexpr int BK = NB <= 4 ? 64 : 32;
-  static constexpr int TILE = BK * RowTile<NB>::P, LDS = 4 * TILE;
+  static constexpr int BK = NB <= 4 ? 64 : 32, STAGES = 2;
+  static constexpr int TILE = BK * RowTile<NB>::P, LDS = STAGES * 2 * TILE;
 };
 
 // Fragments of rows that are on their way from LDS to the matrix core.
 template <int NB>
 constexpr int kAhead = NB == 1 ? 2 : 4;
+
+// step(integral_constant<int, buffer>, key) for every tile, the buffers in turn
+template <int STAGES, class F>
+__device__ __forceinline__ void for_stages(int begin, int end, int tile, F step) {
+  for (int key = begin; key < end; key += STAGES * tile) {
+    step(std::integral_constant<int, 0>{}, key);
+    if (key + tile < end) step(std::integral_constant<int, 1>{}, key + tile);
+    if constexpr (STAGES > 2) {
+      if (key + 2 * tile < end) step(std::integral_constant<int, 2>{}, key + 2 * tile);
+      if (key + 3 * tile < end) step(std::integral_constant<int, 3>{}, key + 3 * tile);
+    }
+  }
+  if constexpr (STAGES > 2) tile_landed();      // zeros that were still on their way
+}
 
 // A row's maximum follows its scores only when they outgrow it by 2^kSlack: probabilities are then up to 2^kSlack in between, which FP16 and FP32 hold as exactly,
 // and the sums are hardly ever multiplied again.
@@ -48,11 +94,13 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_fwd_kernel(At
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Items::Item it = a.items.at(blockIdx.x);
-  const int b = it.b, kvh = it.kvh, tile = it.x, split = it.y, head = kvh * a.rep + it.z;
+  if (it.b < 0) return;
+  const int b = it.b, kvh = it.kvh, split = it.y, row0 = it.x * kRows + wave * 32;
   const int n = a.keys_of(b);
   const int begin = split * a.per_split, end = begin + a.per_split < n ? begin + a.per_split : n;
-  const int q = tile * kRows + wave * 32 + l32;
-  const bool on = q < a.sq;
+  // the queries of the heads that share a key head are the rows of its tiles, one head after the other
+  const int nrows = a.rep * a.sq;
+  const bool on = row0 + l32 < nrows;
   const _Float16* K = a.k.p + b * a.k.batch + kvh * a.k.head;
   const _Float16* V = a.v.p + b * a.v.batch + kvh * a.v.head;
 
@@ -65,7 +113,10 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_fwd_kernel(At
   };
   if (begin < end) request(begin, 0);
   v8h qf[2 * NB];
-  load_fragments<NB>(qf, (const _Float16*)((const uint8_t*)(a.q.p + b * a.q.batch + head * a.q.head) + (long)q * a.q.row), on, a.dh, half);
+  {
+    const RowAt mine(a, kvh, row0 + l32);
+    load_fragments<NB>(qf, (const _Float16*)((const uint8_t*)(a.q.p + b * a.q.batch + mine.head * a.q.head) + (long)mine.q * a.q.row), on, a.dh, half);
+  }
   TileReads<NB> at;
   at.init(lane);
 
@@ -162,12 +213,9 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_fwd_kernel(At
     next_mfma<NB>();
     __builtin_amdgcn_sched_barrier(0);
   };
-  for (int key = begin; key < end; key += 2 * BK) {
-    step(std::integral_constant<int, 0>{}, key);
-    if (key + BK < end) step(std::integral_constant<int, 1>{}, key + BK);
-  }
+  for_stages<C::STAGES>(begin, end, BK, step);
   sum = halves_sum(sum);
-  const long row = ((long)b * a.heads + head) * a.sq + q;
+  const long row = RowAt(a, kvh, row0 + l32, true).of_all(a, b);
   if (a.splits > 1) {
     float* out = a.part + split * a.part_stride + row * a.dh;
     if (begin < end) {
@@ -179,51 +227,71 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_fwd_kernel(At
   }
   const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
   const float f = n > 0 ? alpha / sum : 0.0f;
-  store_rows<NB>(lds, acc, f, a.out + b * a.out_batch + head * a.out_head, a.out_row, tile * kRows + wave * 32, a.sq, a.dh, 0, lane, wave);
+  store_rows<NB>(lds, acc, f, row0, RowsOfHeads(a, b, kvh, nrows), a.dh, 0, lane, wave);
   if (a.lse && on && half == 0) a.lse[row] = n > 0 ? __builtin_fmaf(__builtin_amdgcn_logf(sum), kLn2F, m * a.c2 * kLn2F) : -__builtin_inff();
 }
 
-// The parts of split rows: O = a sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s; parts without keys have l_s = 0 and no O_s.  A wave per row.
-__global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows) {
+// The parts of split rows: O = a sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s; parts without keys have l_s = 0 and no O_s.  A wave per row: its lanes read the
+// statistics together, and `1 << log_lanes` of them (16 bytes each) a part's row, so that parts are read side by side.
+__global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows, int log_lanes) {
   const int lane = threadIdx.x & 63;
   const long row = (long)blockIdx.x * kWaves + (threadIdx.x >> 6);
   if (row >= rows) return;
   const long bh = row / a.sq;
   const int q = (int)(row - bh * a.sq), b = (int)(bh / a.heads), head = (int)(bh - (long)b * a.heads);
   const long stat_stride = a.part_stride / a.dh;
-  float m = -__builtin_inff();
-  for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, a.stats[s * stat_stride + row].x);
-  float sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 st = a.stats[s * stat_stride + row];
-    if (st.y == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(st.x - m);
-    sum = __builtin_fmaf(f, st.y, sum);
-    if (4 * lane < a.dh) {
-      const v4f x = *reinterpret_cast<const v4f*>(a.part + s * a.part_stride + row * a.dh + 4 * lane);
+  const int group = lane >> log_lanes, groups = 64 >> log_lanes, col = (lane & ((1 << log_lanes) - 1)) * 4;
+  float m = -__builtin_inff(), sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s0 = 0; s0 < a.splits; s0 += 64) {
+    const float2 mine = s0 + lane < a.splits ? a.stats[(s0 + lane) * stat_stride + row] : make_float2(-__builtin_inff(), 0.0f);
+    const float most = __builtin_fmaxf(m, wave_max(mine.x));
+    // (no key yet: both are -inf)
+    const float old = most == m ? 1.0f : __builtin_amdgcn_exp2f(m - most), f = mine.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mine.x - most);
+    sum = __builtin_fmaf(old, sum, wave_sum(mine.y == 0.0f ? 0.0f : f * mine.y));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(f, x[e], acc[e]);
+    for (int e = 0; e < 4; ++e) acc[e] *= old;
+    m = most;
+    const int here = a.splits - s0 < 64 ? a.splits - s0 : 64;
+    for (int i = 0; i < here; i += 4 * groups) {
+      v4f x[4];
+      float fs[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int s = i + u * groups + group;
+        fs[u] = __shfl(f, s & 63);
+        if (s >= here) fs[u] = 0.0f;
+        x[u] = fs[u] != 0.0f && col < a.dh ? *reinterpret_cast<const v4f*>(a.part + (s0 + s) * a.part_stride + row * a.dh + col) : v4f{};
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(fs[u], x[u][e], acc[e]);
     }
   }
+  for (int step = 1 << log_lanes; step < 64; step <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], step);
   const int n = a.keys_of(b);
   const bool any = sum != 0.0f;      // (NaN: some)
   const float f = any ? (a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n)) / sum : 0.0f;
-  if (4 * lane < a.dh) {
+  if (group == 0 && col < a.dh) {
     const v4h o = {to_half(acc[0] * f), to_half(acc[1] * f), to_half(acc[2] * f), to_half(acc[3] * f)};
-    wt_store(reinterpret_cast<v4h*>(a.out + b * a.out_batch + head * a.out_head + (long)q * a.out_row + 4 * lane), o);
+    wt_store(reinterpret_cast<v4h*>(a.out + b * a.out_batch + head * a.out_head + (long)q * a.out_row + col), o);
   }
   if (a.lse && lane == 0) a.lse[row] = any ? (m + __builtin_amdgcn_logf(sum)) * kLn2F : -__builtin_inff();
 }
 
 // ---- backward: dQ ---------------------------------------------------------------------------------------------------------
-// Comes first and leaves {log2(e) L - log2(a), D} of every query row for dK and dV, {inf, 0} of the rows that fill the last tile: their P is zero.
+// Comes first and leaves {log2(e) L - log2(a), D} of every query row for dK and dV.
 // D from the rounded O is off by 2^-12 |O| / a of dO, which next to dO v of n keys is 2^-12 (sum p^2)^1/2: of few keys as much as dS's own rounding.  Up to kFewKeys
 // keys D is therefore the sum of p dO v itself, from products made twice (2-norm error of dQ, unit normal inputs, 5 to 120 keys: 2.95e-4 to 2.98e-4, two roundings to FP16; of 140 to 400 keys, from O,
 // 3.2e-4 to 3.1e-4).
 constexpr int kFewKeys = 128;
+// Where a tile is one block of keys (dh > 128) three of them are on their way at a time (us: 32 heads of 256, ragged batch of 5, 869 x 528: 166 -> 156; 130 x 1030:
+// 36 -> 33; the forward pass gains nothing by it: 112 -> 117, 26 -> 26).  Requests then go on behind the last tile, for zeros: every wave has as many loads on its way.
 template <int NB>
 struct DqCfg {
-  static constexpr int BK = NB <= 4 ? 64 : 32, TILE = BK * RowTile<NB>::P, LDS = 4 * TILE;
+  static constexpr int BK = NB <= 4 ? 64 : 32, STAGES = NB <= 4 ? 2 : 4, TILE = BK * RowTile<NB>::P, LDS = STAGES * 2 * TILE;
 };
 template <int NB>
 __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(AttendArgs a) {
@@ -233,11 +301,15 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Items::Item it = a.items.at(blockIdx.x);
-  const int b = it.b, kvh = it.kvh, tile = it.x, split = it.y, head = kvh * a.rep + it.z;
+  if (it.b < 0) return;
+  const int b = it.b, kvh = it.kvh, split = it.y, row0 = it.x * kRows + wave * 32;
   const int n = a.keys_of(b);
   const int begin = split * a.per_split, end = begin + a.per_split < n ? begin + a.per_split : n;
-  const int q = tile * kRows + wave * 32 + l32;
-  const bool on = q < a.sq;
+  // the queries of the heads that share a key head are the rows of its tiles, one head after the other
+  const int nrows = a.rep * a.sq;
+  const bool on = row0 + l32 < nrows;
+  const RowAt mine(a, kvh, row0 + l32);
+  const int h = mine.h, q = mine.q, head = mine.head;
   const _Float16* K = a.k.p + b * a.k.batch + kvh * a.k.head;
   const _Float16* V = a.v.p + b * a.v.batch + kvh * a.v.head;
   TileLoads<NB, BK, kThreads> loads;
@@ -247,7 +319,12 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
     loads.request((const uint8_t*)K + (long)key * a.k.row, n - key, a.k.row, a.dh, to, wave);
     loads.request((const uint8_t*)V + (long)key * a.v.row, n - key, a.v.row, a.dh, to + TILE, wave);
   };
-  if (begin < end) request(begin, 0);
+  auto first_requests = [&] {
+#pragma unroll
+    for (int i = 0; i < C::STAGES - 1; ++i)
+      if (begin + i * BK < end || (C::STAGES > 2 && begin < end)) request(begin + i * BK, i);
+  };
+  first_requests();
   v8h qf[2 * NB], gf[2 * NB];
   load_fragments<NB>(qf, (const _Float16*)((const uint8_t*)(a.q.p + b * a.q.batch + head * a.q.head) + (long)q * a.q.row), on, a.dh, half);
   load_fragments<NB>(gf, (const _Float16*)((const uint8_t*)(a.g.p + b * a.g.batch + head * a.g.head) + (long)q * a.g.row), on, a.dh, half);
@@ -294,9 +371,9 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
     if (on) ld.y = halves_sum(dot) / alpha;
   } else if (begin < end) {
     float ps = 0.0f, pd = 0.0f;
-    for (int key = begin, buffer = 0; key < end; key += BK, buffer ^= 1) {
-      tile_landed();
-      if (key + BK < end) request(key + BK, buffer ^ 1);
+    for (int key = begin, buffer = 0; key < end; key += BK, buffer = (buffer + 1) % C::STAGES) {
+      tile_landed<(C::STAGES - 2) * 2 * decltype(loads)::LD>();
+      if (C::STAGES > 2 || key + BK < end) request(key + (C::STAGES - 1) * BK, (buffer + C::STAGES - 1) % C::STAGES);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         v16f s, dp;
@@ -314,16 +391,23 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
     pd = halves_sum(pd);
     if (on) ld.y = pd / ps;
     tile_landed();
-    request(begin, 0);
+    first_requests();
   }
-  if (split == 0 && half == 0 && q < a.sqp) a.rows[row * a.sqp + q] = ld;
+  if (split == 0 && half == 0) {
+    if (a.across) {
+      if (row0 + l32 < a.rows_per_kv) a.rows[a.row_at<true>(b, kvh, 0, row0 + l32)] = ld;
+    } else if (on) {
+      a.rows[a.row_at<false>(b, kvh, h, q)] = ld;
+      if (q == a.sq - 1 && (a.sq & 1)) a.rows[a.row_at<false>(b, kvh, h, a.sq)] = make_float2(0.0f, 0.0f);
+    }
+  }
   v16f acc[NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) acc[j] = zero16();
   auto step = [&](auto buffer, int key) {
-    constexpr int B = decltype(buffer)::value;
-    tile_landed();
-    if (key + BK < end) request(key + BK, B ^ 1);
+    constexpr int B = decltype(buffer)::value, S = C::STAGES;
+    tile_landed<(S - 2) * 2 * decltype(loads)::LD>();
+    if (S > 2 || key + BK < end) request(key + (S - 1) * BK, (B + S - 1) % S);
     const uint8_t* kt = lds + B * 2 * TILE;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
@@ -360,22 +444,19 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  for (int key = begin; key < end; key += 2 * BK) {
-    step(std::integral_constant<int, 0>{}, key);
-    if (key + BK < end) step(std::integral_constant<int, 1>{}, key + BK);
-  }
+  for_stages<C::STAGES>(begin, end, BK, step);
   const float c = a.c2 * kLn2F;
   if (n == 1) {
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[j] = zero16();
   }
   if (a.splits > 1) {
-    float* out = a.part + split * a.part_stride + (row * a.sq + q) * a.dh;
+    float* out = a.part + split * a.part_stride + RowAt(a, kvh, row0 + l32, true).of_all(a, b) * a.dh;
 #pragma unroll
     for (int j = 0; j < NB; ++j) store_block_f32(out, 32 * j, a.dh, on, half, acc[j], c);
     return;
   }
-  store_rows<NB>(lds, acc, c * a.beta, a.out + b * a.out_batch + head * a.out_head, a.out_row, tile * kRows + wave * 32, a.sq, a.dh, 0, lane, wave);
+  store_rows<NB>(lds, acc, c * a.beta, row0, RowsOfHeads(a, b, kvh, nrows), a.dh, 0, lane, wave);
 }
 
 // ---- backward: dK and dV ------------------------------------------------------------------------------------------------------
@@ -390,7 +471,7 @@ struct DkvCfg {
 struct DkvBlock {
   v16f s, dp;
 };
-template <int NB>
+template <int NB, bool ACROSS>
 __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(AttendArgs a) {
   using C = DkvCfg<NB>;
   constexpr int BQ = C::BQ, QB = BQ / 32, TILE = C::TILE, ACC = C::ACC, AHEAD = kAhead<NB>;
@@ -398,12 +479,13 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Items::Item it = a.items.at(blockIdx.x);
+  if (it.b < 0) return;
   const int b = it.b, kvh = it.kvh, tile = it.y, split = it.z, first = it.x * ACC;
   const int n = a.keys_of(b);
   const int key = tile * kRows + wave * 32 + l32;
   const bool on = key < a.sk;
-  // the tiles of the sharing heads' queries, one head after the other; a split takes per_split of them
-  const int qtiles = (a.sq + BQ - 1) / BQ, total = a.rep * qtiles;
+  // the tiles of the sharing heads' queries, one head after the other, each with tiles of its own or all in the same ones (across); a split takes per_split of them
+  const int nrows = a.rep * a.sq, qtiles = ACROSS ? (nrows + BQ - 1) / BQ : (a.sq + BQ - 1) / BQ, total = ACROSS ? qtiles : a.rep * qtiles;
   const int begin = split * a.per_split;
   int end = begin + a.per_split < total ? begin + a.per_split : total;
   if (tile * kRows >= n) end = begin;
@@ -415,9 +497,20 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
   auto request = [&](int buffer) {
     const int head = kvh * a.rep + rhead, q0 = rtile * BQ;
     uint8_t* to = lds + buffer * C::STAGE;
-    lq.request((const uint8_t*)(a.q.p + b * a.q.batch + head * a.q.head) + (long)q0 * a.q.row, a.sq - q0, a.q.row, a.dh, to, wave);
-    lg.request((const uint8_t*)(a.g.p + b * a.g.batch + head * a.g.head) + (long)q0 * a.g.row, a.sq - q0, a.g.row, a.dh, to + TILE, wave);
-    if (wave == 0) load_to_lds(buffer_words(a.rows + ((long)b * a.heads + head) * a.sqp + q0, BQ * 8), to + 2 * TILE, (uint32_t)lane * 16);
+    const _Float16 *Q = a.q.p + b * a.q.batch + head * a.q.head, *G = a.g.p + b * a.g.batch + head * a.g.head;
+    if constexpr (ACROSS) {
+      auto across = [&](const _Float16* p, const Side& x, uint8_t* lds_tile) {
+        TileLoads<NB, BQ, kThreads>::request_across(p, q0, nrows, a.by_sq, a.sq, (int)(2 * x.head), x.row, (int)((a.rep - 1) * 2 * x.head) + (a.sq - 1) * x.row + 2 * a.dh, a.dh,
+                                                    lds_tile, wave);
+      };
+      across(Q, a.q, to);
+      across(G, a.g, to + TILE);
+    } else {
+      lq.request((const uint8_t*)Q + (long)q0 * a.q.row, a.sq - q0, a.q.row, a.dh, to, wave);
+      lg.request((const uint8_t*)G + (long)q0 * a.g.row, a.sq - q0, a.g.row, a.dh, to + TILE, wave);
+    }
+    const int left = (ACROSS ? a.rows_per_kv : a.rows_per_head) - q0;
+    if (wave == 0) load_to_lds(buffer_words(a.rows + a.row_at<ACROSS>(b, kvh, rhead, q0), (left < BQ ? left : BQ) * 8), to + 2 * TILE, (uint32_t)lane * 16);
     if (++rtile == qtiles) { rtile = 0; ++rhead; }
   };
   if (begin < end) request(0);
@@ -536,8 +629,9 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
     return;
   }
   const long at_head = b * a.k.batch + kvh * a.k.head;
-  store_rows<ACC>(lds, dk, c * a.beta, a.dk + at_head, a.k.row / 2, tile * kRows + wave * 32, a.sk, a.dh, 32 * first, lane, wave);
-  store_rows<ACC>(lds, dv, a.beta, a.dv + at_head, a.k.row / 2, tile * kRows + wave * 32, a.sk, a.dh, 32 * first, lane, wave);
+  const RowsOf dk_rows{(uint8_t*)(a.dk + at_head), a.k.row, a.sk}, dv_rows{(uint8_t*)(a.dv + at_head), a.k.row, a.sk};
+  store_rows<ACC>(lds, dk, c * a.beta, tile * kRows + wave * 32, dk_rows, a.dh, 32 * first, lane, wave);
+  store_rows<ACC>(lds, dv, a.beta, tile * kRows + wave * 32, dv_rows, a.dh, 32 * first, lane, wave);
 }
 
 // Sums of split gradients, part after part: `rows` rows of dh columns `row_stride` elements apart in a part; row = (batch * heads + head) * s + t.
@@ -573,9 +667,6 @@ auto with_blocks(long dh, F f) {
   return f(std::integral_constant<int, 8>{});
 }
 
-// (rows of a tile of queries)
-long padded_rows(long sq) { return (sq + 63) / 64 * 64; }
-
 Side side(const void* p, const us_heads_layout& l) { return Side{(const _Float16*)p, l.batch, l.head, (int)(2 * l.row)}; }
 
 AttendArgs cross_args(const CrossCall& c) {
@@ -591,7 +682,7 @@ AttendArgs cross_args(const CrossCall& c) {
   a.kv = (int)c.kv_heads;
   a.rep = (int)(c.heads / c.kv_heads);
   a.sq = (int)c.sq;
-  a.sqp = (int)padded_rows(c.sq);
+  a.by_sq = FastDiv::by((uint32_t)(c.sq > 0 ? c.sq : 1));
   a.sk = (int)c.sk;
   a.dh = (int)c.dh;
   a.c2 = (float)(1.0 / sqrt((double)c.dh) * 1.44269504088896340736);
@@ -614,22 +705,39 @@ Cut cut(long items, long steps, long least) {
   const long per = steps > 0 ? ceil_div(steps, splits) : 1;
   return {steps > 0 ? (int)ceil_div(steps, per) : 1, per};
 }
-Cut fwd_cut(const CrossCall& c) { return cut(c.batch * c.heads * ceil_div(c.sq, kRows), ceil_div(c.sk, 64), 4); }
-Cut dq_cut(const CrossCall& c) { return cut(c.batch * c.heads * ceil_div(c.sq, kRows), ceil_div(c.sk, 64), 4); }
+long row_tiles(const CrossCall& c) { return ceil_div(c.heads / c.kv_heads * c.sq, kRows); }
+Cut fwd_cut(const CrossCall& c) { return cut(c.batch * c.kv_heads * row_tiles(c), ceil_div(c.sk, 64), 4); }
+Cut dq_cut(const CrossCall& c) { return fwd_cut(c); }
+// How dK's and dV's workgroups take the queries: tiles of each head, or of all heads that share a key head, where that makes fewer tiles and 31 bits hold the
+// heads' distances (us: batch 4, 24 heads by 8 key heads of 80, 2 queries over 12283 keys 72 -> 28; 8 by 4 of 96, 644 queries, 22 tiles or 21: 59 or 62).
+struct QueryTiles {
+  bool across;
+  long tiles;              // of a key head
+  long per_head, per_kv;   // rows of `rows`
+};
+QueryTiles query_tiles(const CrossCall& c, int bq) {
+  const long rep = c.heads / c.kv_heads, own = rep * ceil_div(c.sq, bq), all = ceil_div(rep * c.sq, bq);
+  const long most = c.lq.head > c.lo.head ? c.lq.head : c.lo.head, row = c.lq.row > c.lo.row ? c.lq.row : c.lo.row;
+  const bool fits = 2 * ((rep - 1) * most + c.sq * row) < (1l << 30);
+  if (8 * all <= 7 * own && fits) return {true, all, 0, (rep * c.sq + 1) / 2 * 2};      // (even: loads of 16 bytes)
+  const long per = (c.sq + 1) / 2 * 2;
+  return {false, own, per, rep * per};
+}
 Cut dkv_cut(const CrossCall& c) {
   return with_blocks(c.dh, [&](auto nb) {
     using C = DkvCfg<decltype(nb)::value>;
-    return cut(C::HALVES * c.batch * c.kv_heads * ceil_div(c.sk, kRows), c.heads / c.kv_heads * ceil_div(c.sq, C::BQ), 256 / C::BQ);
+    return cut(C::HALVES * c.batch * c.kv_heads * ceil_div(c.sk, kRows), query_tiles(c, C::BQ).tiles, 256 / C::BQ);
   });
 }
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-size_t rows_bytes(const CrossCall& c) { return up256((size_t)c.batch * c.heads * padded_rows(c.sq) * 8); }
+// (the larger of both ways, which the layouts choose from)
+size_t rows_bytes(const CrossCall& c) { return up256((size_t)c.batch * c.heads * ((c.sq + 1) / 2 * 2) * 8); }
 
 template <class K>
-hipError_t launch(K kernel, FuncConfig& config, long blocks, int lds, const AttendArgs& a, hipStream_t st) {
+hipError_t launch(K kernel, FuncConfig& config, int lds, const AttendArgs& a, hipStream_t st) {
   if (const hipError_t e = config.ensure((const void*)kernel, lds); e != hipSuccess) return e;
-  kernel<<<(unsigned)blocks, kThreads, lds, st>>>(a);
+  kernel<<<a.items.blocks, kThreads, lds, st>>>(a);
   return hipGetLastError();
 }
 
@@ -650,7 +758,9 @@ size_t cross_bwd_workspace_bytes(const CrossCall& c) {
 
 hipError_t launch_join(const AttendArgs& a, hipStream_t st) {
   const long rows = (long)a.batch * a.heads * a.sq;
-  join_kernel<<<(unsigned)ceil_div(rows, kWaves), kThreads, 0, st>>>(a, rows);
+  int log_lanes = 1;
+  while ((4 << log_lanes) < a.dh) ++log_lanes;
+  join_kernel<<<(unsigned)ceil_div(rows, kWaves), kThreads, 0, st>>>(a, rows, log_lanes);
   return hipGetLastError();
 }
 
@@ -662,7 +772,6 @@ hipError_t launch_cross_fwd(const CrossCall& c, void* workspace, hipStream_t st)
   a.out_row = c.lo.row;
   a.lse = c.lse;
   if (few_rows_take(c.heads, c.kv_heads, c.sq)) return launch_few_rows(a, workspace, st);
-  a.tiles = (int)ceil_div(c.sq, kRows);
   Cut s = fwd_cut(c);
   if (!workspace) s = {1, ceil_div(c.sk, 64)};
   a.splits = s.splits;
@@ -674,8 +783,8 @@ hipError_t launch_cross_fwd(const CrossCall& c, void* workspace, hipStream_t st)
   const hipError_t e = with_blocks(c.dh, [&](auto nb) {
     constexpr int NB = decltype(nb)::value;
     static FuncConfig config;
-    a.items = Items::of(c.batch * c.kv_heads, c.kv_heads, a.tiles, a.splits, a.rep, device_info().xcds);
-    return launch(cross_fwd_kernel<NB>, config, c.batch * c.heads * a.tiles * a.splits, FwdCfg<NB>::LDS, a, st);
+    a.items = Items::of(c.batch * c.kv_heads, c.kv_heads, row_tiles(c), a.splits, 1, device_info().xcds);
+    return launch(cross_fwd_kernel<NB>, config, FwdCfg<NB>::LDS, a, st);
   });
   if (e != hipSuccess || a.splits == 1) return e;
   return launch_join(a, st);
@@ -687,6 +796,10 @@ hipError_t launch_cross_bwd(const CrossCall& c, void* dQ, void* dK, void* dV, fl
   a.rows = (float2*)workspace;
   a.part = (float*)((uint8_t*)workspace + rows_bytes(c));
   a.lse = c.lse;
+  const QueryTiles qt = with_blocks(c.dh, [&](auto nb) { return query_tiles(c, DkvCfg<decltype(nb)::value>::BQ); });
+  a.across = qt.across;
+  a.rows_per_head = (int)qt.per_head;
+  a.rows_per_kv = (int)qt.per_kv;
   if (c.sq > 0) {
     AttendArgs q = a;
     q.out = (_Float16*)dQ;
@@ -694,16 +807,15 @@ hipError_t launch_cross_bwd(const CrossCall& c, void* dQ, void* dK, void* dV, fl
     q.out_head = c.lq.head;
     q.out_row = c.lq.row;
     q.beta = beta_q;
-    q.tiles = (int)ceil_div(c.sq, kRows);
     const Cut s = dq_cut(c);
     q.splits = s.splits;
     q.per_split = (int)(s.per * 64);
     q.part_stride = c.batch * c.heads * c.sq * c.dh;
-    q.items = Items::of(c.batch * c.kv_heads, c.kv_heads, q.tiles, q.splits, q.rep, xcds);
+    q.items = Items::of(c.batch * c.kv_heads, c.kv_heads, row_tiles(c), q.splits, 1, xcds);
     hipError_t e = with_blocks(c.dh, [&](auto nb) {
       constexpr int NB = decltype(nb)::value;
       static FuncConfig config;
-      return launch(cross_dq_kernel<NB>, config, c.batch * c.heads * q.tiles * q.splits, DqCfg<NB>::LDS, q, st);
+      return launch(cross_dq_kernel<NB>, config, DqCfg<NB>::LDS, q, st);
     });
     if (e != hipSuccess) return e;
     if (q.splits > 1) {
@@ -725,9 +837,9 @@ hipError_t launch_cross_bwd(const CrossCall& c, void* dQ, void* dK, void* dV, fl
     constexpr int NB = decltype(nb)::value;
     using C = DkvCfg<NB>;
     static FuncConfig config;
-    a.tiles = (int)ceil_div(c.sk, kRows);
-    a.items = Items::of(c.batch * c.kv_heads, c.kv_heads, C::HALVES, a.tiles, a.splits, xcds);
-    return launch(cross_dkv_kernel<NB>, config, C::HALVES * c.batch * c.kv_heads * a.tiles * a.splits, C::LDS, a, st);
+    a.items = Items::of(c.batch * c.kv_heads, c.kv_heads, C::HALVES, ceil_div(c.sk, kRows), a.splits, xcds);
+    static FuncConfig across;
+    return qt.across ? launch(cross_dkv_kernel<NB, true>, across, C::LDS, a, st) : launch(cross_dkv_kernel<NB, false>, config, C::LDS, a, st);
   });
   if (e != hipSuccess || a.splits == 1) return e;
   const long rows = c.batch * c.kv_heads * c.sk;

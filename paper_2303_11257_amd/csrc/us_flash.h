@@ -77,8 +77,12 @@ struct TileReads {
 __device__ __forceinline__ void load_to_lds(v4i from, uint8_t* lds, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)US_LDS_AT(uint8_t, lds)), "v"(off), "s"(from) : "memory");
 }
-// All loads of the workgroup to LDS have landed, all its reads of LDS are done; nothing that reads or writes memory moves across.
-__device__ __forceinline__ void tile_landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All loads of the workgroup to LDS but each wave's newest N have landed, all its reads of LDS are done; nothing that reads or writes memory moves across.
+template <int N = 0>
+__device__ __forceinline__ void tile_landed() {
+  static_assert(N >= 0 && N < 64, "");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
 
 // The loads of a tile of ROWS rows by THREADS threads, straight to LDS; rows from `rows` on and columns from dh on are zeros.
 template <int NB, int ROWS, int THREADS>
@@ -92,6 +96,20 @@ struct TileLoads {
       const int o = (j * THREADS + (int)threadIdx.x) * 16, row = o / T::P, chunk = ((o % T::P) >> 4) ^ T::swz(row);
       off[j] = chunk * 8 < dh ? (uint32_t)(row * row_bytes + chunk * 16) : 0x7ffffff0u;
     }
+  }
+  // the tile's rows are rows r0 .. of several heads one after the other (by_s divides by a head's s rows), `head_bytes` apart, `rows` in all; the whole lies
+  // within 31 bits of `base`
+  __device__ __forceinline__ static void request_across(const void* base, int r0, int rows, FastDiv by_s, int s, int head_bytes, int row_bytes, int bytes, int dh,
+                                                        uint8_t* lds, int wave) {
+    const v4i res = buffer_words(base, (uint32_t)bytes);
+#pragma unroll
+    for (int j = 0; j < LD; ++j)
+      if (BYTES / 16 % THREADS == 0 || j * THREADS + wave * 64 < BYTES / 16) {
+        const int o = (j * THREADS + (int)threadIdx.x) * 16, row = o / T::P, chunk = ((o % T::P) >> 4) ^ T::swz(row), r = r0 + row;
+        const int h = (int)by_s.of((uint32_t)r);
+        const uint32_t at = (uint32_t)(h * head_bytes + (r - h * s) * row_bytes + chunk * 16);
+        load_to_lds(res, lds + (j * THREADS + wave * 64) * 16, r < rows && chunk * 8 < dh ? at : 0x7ffffff0u);
+      }
   }
   __device__ __forceinline__ void request(const void* base, long rows, int row_bytes, int dh, uint8_t* lds, int wave) const {
     const int r = rows > ROWS ? ROWS : rows < 0 ? 0 : (int)rows;
@@ -135,11 +153,10 @@ __device__ __forceinline__ v4i eight_columns(const v16f& x, int k, float f) {
   return o;
 }
 // A wave's 32 rows of COLS blocks of 32 columns (from column `col0` on) to memory, through LDS: whole rows at a time.  From the registers a store would write 32 bytes
-// of each row, and memory takes such pieces at a fraction of its rate (16 x 16 heads of 64, 512 queries over up to 1024 keys: dK and dV 92 -> 73 us, O 41 -> 34).  Every wave of the workgroup calls it; rows from `rows` on and columns from dh on
-// stay as they are.
-template <int COLS>
-__device__ __forceinline__ void store_rows(uint8_t* lds, const v16f (&x)[COLS], float f, _Float16* base, long row_stride, int row0, int rows, int dh, int col0, int lane,
-                                           int wave) {
+// of each row, and memory takes such pieces at a fraction of its rate (16 x 16 heads of 64, 512 queries over up to 1024 keys: dK and dV 92 -> 73 us, O 41 -> 34).  Every wave of the workgroup calls it; columns from dh on stay as they are.
+// row_of(r): where row r (of 32 from row0 on) starts, or NULL
+template <int COLS, class R>
+__device__ __forceinline__ void store_rows(uint8_t* lds, const v16f (&x)[COLS], float f, int row0, R row_of, int dh, int col0, int lane, int wave) {
   constexpr int G = COLS <= 4 ? COLS : COLS / 2, PITCH = 64 * G + 16;      // blocks at a time
   uint8_t* mine = lds + wave * 32 * PITCH;
 #pragma unroll
@@ -154,7 +171,8 @@ __device__ __forceinline__ void store_rows(uint8_t* lds, const v16f (&x)[COLS], 
     for (int i = 0; i < 2 * G; ++i) {
       const int c = i * 64 + lane, row = c / (4 * G), chunk = c - row * (4 * G), col = col0 + 32 * g + 8 * chunk;
       const v4i o = *US_LDS_AT(const v4i, mine + row * PITCH + chunk * 16);
-      if (row0 + row < rows && col < dh) wt_store(reinterpret_cast<v4i*>(base + (row0 + row) * row_stride + col), o);
+      _Float16* const to = row_of(row0 + row);
+      if (to && col < dh) wt_store(reinterpret_cast<v4i*>(to + col), o);
     }
   }
 }
@@ -171,10 +189,15 @@ __device__ __forceinline__ void store_block_f32(float* row, int col0, int dh, bo
 // evenly.  The host prepares the divisions.
 struct Items {
   FastDiv by_xcds, by_per, by_x, by_y, by_kv;
-  uint32_t xcds, per, nx, ny, kv;
+  uint32_t xcds, per, nx, ny, kv, groups, blocks;
   static Items of(long groups, long kv, long nx, long ny, long nz, int xcds) {
     Items i;
-    i.xcds = groups % xcds == 0 ? (uint32_t)xcds : 1u;
+    // Not where a group is one workgroup, which has nothing to share (54 x 53 heads of 128, 3 x 184, dQ: 60 us in order, 69 by XCD).  A few idle workgroups even the
+    // groups out (124 heads of 2943 x 2909 x 128, dK and dV: 1560 us in order, 1460 with 128 groups).
+    const long even = (groups + xcds - 1) / xcds * xcds;
+    i.xcds = even * 10 <= groups * 11 && nx * ny * nz > 1 ? (uint32_t)xcds : 1u;
+    i.groups = (uint32_t)groups;
+    i.blocks = (uint32_t)((i.xcds > 1 ? even : groups) * nx * ny * nz);
     i.per = (uint32_t)(nx * ny * nz);
     i.nx = (uint32_t)nx;
     i.ny = (uint32_t)ny;
@@ -187,7 +210,7 @@ struct Items {
     return i;
   }
   struct Item {
-    int b, kvh, x, y, z;
+    int b, kvh, x, y, z;      // b < 0: nothing to do
   };
   __device__ __forceinline__ Item at(uint32_t block) const {
     const uint32_t i = by_xcds.of(block), xcd = block - i * xcds, q = by_per.of(i), group = q * xcds + xcd;
@@ -195,6 +218,7 @@ struct Items {
     Item it;
     it.b = (int)by_kv.of(group);
     it.kvh = (int)(group - (uint32_t)it.b * kv);
+    if (group >= groups) it.b = -1;
     const uint32_t rx = by_x.of(r), ry = by_y.of(rx);
     it.x = (int)(r - rx * nx);
     it.y = (int)(rx - ry * ny);
@@ -221,19 +245,27 @@ struct AttendArgs {
   _Float16 *out, *dk, *dv;  // O or dQ (out_batch ..), dK and dV (laid out as k)
   long out_batch, out_head, out_row;
   float* lse;               // forward: L, or NULL
-  float2* rows;             // backward: {log2(e) L - log2(a), D} of [batch * heads][sqp]
+  float2* rows;             // backward: {log2(e) L - log2(a), D} of [batch * kv][rows_per_kv]
   float* part;              // parts of split sums
   float2* stats;            // forward: {largest score (base 2), sum} of a part's rows
   long part_stride;         // elements between parts
   Items items;
-  int batch, heads, kv, rep, sq, sqp, sk, dh, tiles, splits, per_split;
+  FastDiv by_sq;
+  int batch, heads, kv, rep, sq, sk, dh, splits, per_split, tiles;      // tiles: of 16 rows (us_paged.hip)
+  // backward: rows of `rows` per key head; whether a tile of queries goes on in the next head; a head's rows in `rows` where it does not
+  int rows_per_kv, rows_per_head;
+  bool across;
+  // the row of `rows` of query q of the h-th head of a key head; across: of row q of the key head
+  template <bool ACROSS>
+  __device__ __forceinline__ long row_at(int b, int kvh, int h, int q) const {
+    return ((long)b * kv + kvh) * rows_per_kv + (ACROSS ? q : h * rows_per_head + q);
+  }
   float c2, alpha, beta;    // c2 = dh^-1/2 log2(e);  alpha <= 0: n^1/2;  beta: factor of the gradient's store
   __device__ __forceinline__ int keys_of(int b) const {
     const int n = klen ? klen[b] : sk;
     return n < 0 ? 0 : n > sk ? sk : n;
   }
 };
-hipError_t launch_join(const AttendArgs& a, hipStream_t st);      // us_cross.hip
 // The forward pass where a key head has few rows (us_paged.hip).
 bool few_rows_take(long heads, long kv_heads, long sq);
 size_t few_rows_workspace_bytes(long batch, long heads, long kv, long sq, long sk, long dh);
