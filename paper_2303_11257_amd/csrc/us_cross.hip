@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
       lq.request((const uint8_t*)Q + (long)q0 * a.q.row, a.sq - q0, a.q.row, a.dh, to, wave);
       lg.request((const uint8_t*)G + (long)q0 * a.g.row, a.sq - q0, a.g.row, a.dh, to + TILE, wave);
     }
-    const int left = (ACROSS ? a.rows_per_kv : a.rows_per_head) - q0;
+    const int left = (((ACROSS ? nrows : a.sq) + 1) & ~1) - q0;      // (loads of 16 bytes take two rows; zeros behind them, as Q and dO are there)
     if (wave == 0) load_to_lds(buffer_words(a.rows + a.row_at<ACROSS>(b, kvh, rhead, q0), (left < BQ ? left : BQ) * 8), to + 2 * TILE, (uint32_t)lane * 16);
     if (++rtile == qtiles) { rtile = 0; ++rhead; }
   };
@@ -719,8 +719,8 @@ QueryTiles query_tiles(const CrossCall& c, int bq) {
   const long rep = c.heads / c.kv_heads, own = rep * ceil_div(c.sq, bq), all = ceil_div(rep * c.sq, bq);
   const long most = c.lq.head > c.lo.head ? c.lq.head : c.lo.head, row = c.lq.row > c.lo.row ? c.lq.row : c.lo.row;
   const bool fits = 2 * ((rep - 1) * most + c.sq * row) < (1l << 30);
-  if (8 * all <= 7 * own && fits) return {true, all, 0, (rep * c.sq + 1) / 2 * 2};      // (even: loads of 16 bytes)
-  const long per = (c.sq + 1) / 2 * 2;
+  if (8 * all <= 7 * own && fits) return {true, all, 0, (rep * c.sq + 31) / 32 * 32};      // (whole lines)
+  const long per = (c.sq + 31) / 32 * 32;
   return {false, own, per, rep * per};
 }
 Cut dkv_cut(const CrossCall& c) {
@@ -732,7 +732,7 @@ Cut dkv_cut(const CrossCall& c) {
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // (the larger of both ways, which the layouts choose from)
-size_t rows_bytes(const CrossCall& c) { return up256((size_t)c.batch * c.heads * ((c.sq + 1) / 2 * 2) * 8); }
+size_t rows_bytes(const CrossCall& c) { return up256((size_t)c.batch * c.heads * ((c.sq + 31) / 32 * 32) * 8); }
 
 template <class K>
 hipError_t launch(K kernel, FuncConfig& config, int lds, const AttendArgs& a, hipStream_t st) {
