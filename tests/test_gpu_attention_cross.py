@@ -180,6 +180,32 @@ def test_forward_without_workspace_or_lse(dims):
     R.close(c.t["O"], c.reference(False)["O"], "O")
 
 
+@pytest.mark.parametrize("layout", ["packed", "tokens", "gaps"])
+@pytest.mark.parametrize("dims", [(3, 10, 5, 37, 300, 64), (2, 12, 3, 21, 150, 160), (1, 9, 3, 43, 700, 256), (3, 30, 2, 3, 260, 96), (5, 14, 2, 33, 90, 16), (1, 24, 1, 129, 40, 128)], ids=str)
+def test_heads_that_share_keys_also_share_tiles(dims, layout):
+    """Queries of a key head's heads in the same tiles, a tile over two and over many heads, key heads that no number of XCDs divides, ragged keys."""
+    c = Call(*dims, klen=[dims[4] - 57 * b % dims[4] for b in range(dims[0])], layout=layout, seed=8, fill=float("nan"))
+    c.fwd()
+    c.bwd()
+    c.check(what=f"{layout} ")
+
+
+def test_a_bad_query_beside_other_heads_in_its_tile():
+    c = Call(1, 8, 2, 20, 150, 64, seed=6)
+    c.Q[0, 5, 13, 5] = float("nan")
+    c.t["Q"].copy_(c.Q)
+    c.fwd()
+    c.bwd()
+    bad = torch.zeros(1, 8, 20, dtype=torch.bool)
+    bad[0, 5, 13] = True
+    for name in ("O", "dQ"):
+        got = c.t[name].float().cpu()
+        assert bool(got[bad].isnan().all()) and bool(got[~bad].isfinite().all()), name
+    for name in ("dK", "dV"):
+        got = c.t[name].float().cpu()
+        assert bool(got[0, 1].isnan().all()) and bool(got[0, 0].isfinite().all()), name
+
+
 def test_items_that_share_keys():
     """A batch stride of zero: several sequences over one encoder's states."""
     batch, heads, sq, sk, dh = 3, 2, 21, 100, 64
