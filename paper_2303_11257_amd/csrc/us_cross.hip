@@ -25,18 +25,24 @@ __device__ __forceinline__ void load_fragments(v8h (&f)[2 * NB], const _Float16*
   }
 }
 
-// Row r of a key head: query q of its h-th head.  `again`: worked out anew, so that no register holds it through the loop over the keys (the forward kernel of 64
-// columns, 512 x 1024: 130 registers a lane and three waves a SIMD 38 us, 128 and four 34).
+// Row r of a key head: query q of its h-th head.
 struct RowAt {
   int h, q, head;
-  __device__ __forceinline__ RowAt(const AttendArgs& a, int kvh, int r, bool again = false) {
-    if (again) asm volatile("" : "+v"(r));
+  __device__ __forceinline__ RowAt(const AttendArgs& a, int kvh, int r) {
     h = (int)a.by_sq.of((uint32_t)r);
     q = r - h * a.sq;
     head = kvh * a.rep + h;
   }
   __device__ __forceinline__ long of_all(const AttendArgs& a, int b) const { return ((long)b * a.heads + head) * a.sq + q; }
 };
+// The lane, and its row of a wave's 32 from row0 on, worked out anew: no register holds it through the loop over the keys (the forward kernel of 64 columns, 512 x 1024: 130
+// registers a lane and three waves a SIMD 38 us, 126 and four 34).
+__device__ __forceinline__ int lane_again() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t & 63;
+}
+__device__ __forceinline__ int row_again(int row0) { return row0 + (lane_again() & 31); }
 // Where the rows of a key head's O or dQ start, and those of dK or dV.  (No reference to the kernel's arguments: those are then no longer scalars.)
 struct RowsOfHeads {
   FastDiv by_sq;
@@ -95,7 +101,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_fwd_kernel(At
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Items::Item it = a.items.at(blockIdx.x);
   if (it.b < 0) return;
-  const int b = it.b, kvh = it.kvh, split = it.y, row0 = it.x * kRows + wave * 32;
+  const int b = a.by_keys(it.b), kvh = it.kvh, split = it.y, row0 = it.x * kRows + wave * 32;
   const int n = a.keys_of(b);
   const int begin = split * a.per_split, end = begin + a.per_split < n ? begin + a.per_split : n;
   // the queries of the heads that share a key head are the rows of its tiles, one head after the other
@@ -215,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_fwd_kernel(At
   };
   for_stages<C::STAGES>(begin, end, BK, step);
   sum = halves_sum(sum);
-  const long row = RowAt(a, kvh, row0 + l32, true).of_all(a, b);
+  const long row = RowAt(a, kvh, row_again(row0)).of_all(a, b);
   if (a.splits > 1) {
     float* out = a.part + split * a.part_stride + row * a.dh;
     if (begin < end) {
@@ -287,6 +293,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows,
 // keys D is therefore the sum of p dO v itself, from products made twice (2-norm error of dQ, unit normal inputs, 5 to 120 keys: 2.95e-4 to 2.98e-4, two roundings to FP16; of 140 to 400 keys, from O,
 // 3.2e-4 to 3.1e-4).
 constexpr int kFewKeys = 128;
+// Heads of up to 64 columns: 124 registers a lane, so four waves a SIMD.
 // Where a tile is one block of keys (dh > 128) three of them are on their way at a time (us: 32 heads of 256, ragged batch of 5, 869 x 528: 166 -> 156; 130 x 1030:
 // 36 -> 33; the forward pass gains nothing by it: 112 -> 117, 26 -> 26).  Requests then go on behind the last tile, for zeros: every wave has as many loads on its way.
 template <int NB>
@@ -294,7 +301,7 @@ struct DqCfg {
   static constexpr int BK = NB <= 4 ? 64 : 32, STAGES = NB <= 4 ? 2 : 4, TILE = BK * RowTile<NB>::P, LDS = STAGES * 2 * TILE;
 };
 template <int NB>
-__global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, NB <= 2 ? 4 : NB <= 4 ? 2 : 1) cross_dq_kernel(AttendArgs a) {
   using C = DqCfg<NB>;
   constexpr int BK = C::BK, KB = BK / 32, TILE = C::TILE;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -302,14 +309,12 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Items::Item it = a.items.at(blockIdx.x);
   if (it.b < 0) return;
-  const int b = it.b, kvh = it.kvh, split = it.y, row0 = it.x * kRows + wave * 32;
+  const int b = a.by_keys(it.b), kvh = it.kvh, split = it.y, row0 = it.x * kRows + wave * 32;
   const int n = a.keys_of(b);
   const int begin = split * a.per_split, end = begin + a.per_split < n ? begin + a.per_split : n;
   // the queries of the heads that share a key head are the rows of its tiles, one head after the other
   const int nrows = a.rep * a.sq;
   const bool on = row0 + l32 < nrows;
-  const RowAt mine(a, kvh, row0 + l32);
-  const int h = mine.h, q = mine.q, head = mine.head;
   const _Float16* K = a.k.p + b * a.k.batch + kvh * a.k.head;
   const _Float16* V = a.v.p + b * a.v.batch + kvh * a.v.head;
   TileLoads<NB, BK, kThreads> loads;
@@ -326,8 +331,11 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
   };
   first_requests();
   v8h qf[2 * NB], gf[2 * NB];
-  load_fragments<NB>(qf, (const _Float16*)((const uint8_t*)(a.q.p + b * a.q.batch + head * a.q.head) + (long)q * a.q.row), on, a.dh, half);
-  load_fragments<NB>(gf, (const _Float16*)((const uint8_t*)(a.g.p + b * a.g.batch + head * a.g.head) + (long)q * a.g.row), on, a.dh, half);
+  {
+    const RowAt mine(a, kvh, row0 + l32);
+    load_fragments<NB>(qf, (const _Float16*)((const uint8_t*)(a.q.p + b * a.q.batch + mine.head * a.q.head) + (long)mine.q * a.q.row), on, a.dh, half);
+    load_fragments<NB>(gf, (const _Float16*)((const uint8_t*)(a.g.p + b * a.g.batch + mine.head * a.g.head) + (long)mine.q * a.g.row), on, a.dh, half);
+  }
   TileReads<NB> at;
   at.init(lane);
   constexpr int AHEAD = kAhead<NB>, CA = NB <= 4 ? NB : 4;
@@ -347,18 +355,19 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
   };
   auto mask = [&](v16f& s, int key) {
     if (key + 32 > end) {
+      const int first = key + 4 * (lane_again() >> 5);
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (key + 8 * (r / 4) + 4 * half + r % 4 >= end) s[r] = -__builtin_inff();
+        if (first + 8 * (r / 4) + r % 4 >= end) s[r] = -__builtin_inff();
     }
   };
-  const long row = (long)b * a.heads + head;
   float2 ld = make_float2(__builtin_inff(), 0.0f);
   const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
-  if (on && n > 0) ld.x = __builtin_fmaf(a.lse[row * a.sq + q], kLog2eF, -__builtin_amdgcn_logf(alpha));
+  if (on && n > 0) ld.x = __builtin_fmaf(a.lse[RowAt(a, kvh, row_again(row0)).of_all(a, b)], kLog2eF, -__builtin_amdgcn_logf(alpha));
   if (n > kFewKeys) {
     float dot = 0.0f;
-    const _Float16* o = (const _Float16*)((const uint8_t*)(a.o.p + b * a.o.batch + head * a.o.head) + (long)q * a.o.row);
+    const RowAt mine(a, kvh, row_again(row0));
+    const _Float16* o = (const _Float16*)((const uint8_t*)(a.o.p + b * a.o.batch + mine.head * a.o.head) + (long)mine.q * a.o.row);
 #pragma unroll
     for (int t = 0; t < 2 * NB; ++t) {
       const int col = 16 * t + 8 * half;
@@ -393,12 +402,14 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
     tile_landed();
     first_requests();
   }
-  if (split == 0 && half == 0) {
+  if (split == 0 && lane_again() < 32) {
     if (a.across) {
-      if (row0 + l32 < a.rows_per_kv) a.rows[a.row_at<true>(b, kvh, 0, row0 + l32)] = ld;
+      const int r = row_again(row0);
+      if (r < a.rows_per_kv) a.rows[a.row_at<true>(b, kvh, 0, r)] = ld;
     } else if (on) {
-      a.rows[a.row_at<false>(b, kvh, h, q)] = ld;
-      if (q == a.sq - 1 && (a.sq & 1)) a.rows[a.row_at<false>(b, kvh, h, a.sq)] = make_float2(0.0f, 0.0f);
+      const RowAt mine(a, kvh, row_again(row0));
+      a.rows[a.row_at<false>(b, kvh, mine.h, mine.q)] = ld;
+      if (mine.q == a.sq - 1 && (a.sq & 1)) a.rows[a.row_at<false>(b, kvh, mine.h, a.sq)] = make_float2(0.0f, 0.0f);
     }
   }
   v16f acc[NB];
@@ -451,12 +462,12 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_dq_kernel(Att
     for (int j = 0; j < NB; ++j) acc[j] = zero16();
   }
   if (a.splits > 1) {
-    float* out = a.part + split * a.part_stride + RowAt(a, kvh, row0 + l32, true).of_all(a, b) * a.dh;
+    float* out = a.part + split * a.part_stride + RowAt(a, kvh, row_again(row0)).of_all(a, b) * a.dh;
 #pragma unroll
-    for (int j = 0; j < NB; ++j) store_block_f32(out, 32 * j, a.dh, on, half, acc[j], c);
+    for (int j = 0; j < NB; ++j) store_block_f32(out, 32 * j, a.dh, on, lane_again() >> 5, acc[j], c);
     return;
   }
-  store_rows<NB>(lds, acc, c * a.beta, row0, RowsOfHeads(a, b, kvh, nrows), a.dh, 0, lane, wave);
+  store_rows<NB>(lds, acc, c * a.beta, row0, RowsOfHeads(a, b, kvh, nrows), a.dh, 0, lane_again(), wave);
 }
 
 // ---- backward: dK and dV ------------------------------------------------------------------------------------------------------
@@ -489,6 +500,19 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
   const int begin = split * a.per_split;
   int end = begin + a.per_split < total ? begin + a.per_split : total;
   if (tile * kRows >= n) end = begin;
+  const long at_head = b * a.k.batch + kvh * a.k.head;
+  const RowsOf dk_rows{(uint8_t*)(a.dk + at_head), a.k.row, a.sk}, dv_rows{(uint8_t*)(a.dv + at_head), a.k.row, a.sk};
+  if (begin >= end && a.splits == 1) {      // zeros, without the detour through LDS (the same: 73 -> 70 us)
+#pragma unroll
+    for (int i = 0; i < 2 * ACC; ++i) {
+      const int c = i * 64 + lane, row = c / (4 * ACC), col = 32 * first + 8 * (c - row * (4 * ACC)), r = tile * kRows + wave * 32 + row;
+      if (r < a.sk && col < a.dh) {
+        wt_store(reinterpret_cast<v4i*>(dk_rows(r) + col), v4i{});
+        wt_store(reinterpret_cast<v4i*>(dv_rows(r) + col), v4i{});
+      }
+    }
+    return;
+  }
 
   TileLoads<NB, BQ, kThreads> lq, lg;
   lq.init(a.q.row, a.dh);
@@ -628,8 +652,6 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
     }
     return;
   }
-  const long at_head = b * a.k.batch + kvh * a.k.head;
-  const RowsOf dk_rows{(uint8_t*)(a.dk + at_head), a.k.row, a.sk}, dv_rows{(uint8_t*)(a.dv + at_head), a.k.row, a.sk};
   store_rows<ACC>(lds, dk, c * a.beta, tile * kRows + wave * 32, dk_rows, a.dh, 32 * first, lane, wave);
   store_rows<ACC>(lds, dv, a.beta, tile * kRows + wave * 32, dv_rows, a.dh, 32 * first, lane, wave);
 }

@@ -261,6 +261,18 @@ struct AttendArgs {
     return ((long)b * kv + kvh) * rows_per_kv + (ACROSS ? q : h * rows_per_head + q);
   }
   float c2, alpha, beta;    // c2 = dh^-1/2 log2(e);  alpha <= 0: n^1/2;  beta: factor of the gradient's store
+  // The item with the slot-th most keys, of up to 64, which the lanes rank against one another: the longest first, so that the CUs' shares come out even (us: 16 items
+  // of 16 heads of 64, 512 queries, 64 to 1024 keys: forward 35 -> 31, dQ 50 -> 44.  dK and dV, whose workgroups have equal work or none, do without: 70 or 75).
+  __device__ __forceinline__ int by_keys(int slot) const {
+    if (!klen || batch > 64) return slot;
+    const int lane = threadIdx.x & 63, mine = lane < batch ? keys_of(lane) : 0;
+    int rank = 0;
+    for (int j = 0; j < batch; ++j) {
+      const int other = __builtin_amdgcn_readlane(mine, j);
+      rank += other > mine || (other == mine && j < lane) ? 1 : 0;
+    }
+    return __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < batch && rank == slot));
+  }
   __device__ __forceinline__ int keys_of(int b) const {
     const int n = klen ? klen[b] : sk;
     return n < 0 ? 0 : n > sk ? sk : n;
