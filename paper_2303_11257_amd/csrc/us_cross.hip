@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows,
 }
 
 // ---- backward: dQ ---------------------------------------------------------------------------------------------------------
-// Comes first and leaves {log2(e) L - log2(a), D} of every query row for dK and dV.
+// Comes first and leaves what dK and dV need of every query row, log2(e) L - log2(a) and D.
 // D from the rounded O is off by 2^-12 |O| / a of dO, which next to dO v of n keys is 2^-12 (sum p^2)^1/2: of few keys as much as dS's own rounding.  Up to kFewKeys
 // keys D is therefore the sum of p dO v itself, from products made twice (2-norm error of dQ, unit normal inputs, 5 to 120 keys: 2.95e-4 to 2.98e-4, two roundings to FP16; of 140 to 400 keys, from O,
 // 3.2e-4 to 3.1e-4).
@@ -402,15 +402,10 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 4 : NB <= 4 ? 2 : 1) cross
     tile_landed();
     first_requests();
   }
-  if (split == 0 && lane_again() < 32) {
-    if (a.across) {
-      const int r = row_again(row0);
-      if (r < a.rows_per_kv) a.rows[a.row_at<true>(b, kvh, 0, r)] = ld;
-    } else if (on) {
-      const RowAt mine(a, kvh, row_again(row0));
-      a.rows[a.row_at<false>(b, kvh, mine.h, mine.q)] = ld;
-      if (mine.q == a.sq - 1 && (a.sq & 1)) a.rows[a.row_at<false>(b, kvh, mine.h, a.sq)] = make_float2(0.0f, 0.0f);
-    }
+  if (split == 0 && on && lane_again() < 32) {
+    // (infinite L, of rows without keys: large, as zeros times infinity are no zeros)
+    const float l = ld.x / a.c2;
+    a.rows[RowAt(a, kvh, row_again(row0)).of_all(a, b)] = row_stat(l > 1e38f ? 1e38f : l, ld.y);
   }
   v16f acc[NB];
 #pragma unroll
@@ -533,8 +528,8 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
       lq.request((const uint8_t*)Q + (long)q0 * a.q.row, a.sq - q0, a.q.row, a.dh, to, wave);
       lg.request((const uint8_t*)G + (long)q0 * a.g.row, a.sq - q0, a.g.row, a.dh, to + TILE, wave);
     }
-    const int left = (((ACROSS ? nrows : a.sq) + 1) & ~1) - q0;      // (loads of 16 bytes take two rows; zeros behind them, as Q and dO are there)
-    if (wave == 0) load_to_lds(buffer_words(a.rows + a.row_at<ACROSS>(b, kvh, rhead, q0), (left < BQ ? left : BQ) * 8), to + 2 * TILE, (uint32_t)lane * 16);
+    const int left = (ACROSS ? nrows : a.sq) - q0;      // (zeros behind them, as Q and dO are there: P is then 1, and all that it meets 0)
+    if (wave == 0) load_to_lds(buffer_words(a.rows + ((long)b * a.heads + head) * a.sq + q0, (left < BQ ? left : BQ) * 16), to + 2 * TILE, (uint32_t)lane * 16);
     if (++rtile == qtiles) { rtile = 0; ++rhead; }
   };
   if (begin < end) request(0);
@@ -547,9 +542,11 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
 #pragma unroll
   for (int j = 0; j < ACC; ++j) dk[j] = dv[j] = zero16();
 
+  const v4i ones_s = row_ones(false, half), ones_dp = row_ones(true, half);
   auto products = [&](const uint8_t* qt, int qb, DkvBlock& x) {
     // (scores and dO v in turn: a product that adds to the one just before it has to wait for it)
     auto fragment = [&](int i) { return at.rows(i % 2 ? qt + TILE : qt, qb, i / 2); };
+    const v4i stat = *US_LDS_AT(const v4i, qt + 2 * TILE + (qb * 32 + l32) * 16);
     v8h rf[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) rf[i] = fragment(i);
@@ -560,23 +557,19 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
       else x.s = mfma32(rf[i % AHEAD], kf[i / 2], x.s);
       if (i + AHEAD < 4 * NB) rf[i % AHEAD] = fragment(i + AHEAD);
     }
+    x.s = mfma32_bf16(stat, ones_s, x.s);
+    x.dp = mfma32_bf16(stat, ones_dp, x.dp);
   };
   // Block qb of the tile at qt becomes part of the gradients; meanwhile block nqb of the tile at nt is made, so that matrix core and vector ALU both have work.
   auto block = [&](DkvBlock& cur, const uint8_t* qt, int qb, DkvBlock& next, const uint8_t* nt, int nqb) {
-    const uint8_t *gt = qt + TILE, *st = gt + TILE;
-    v4f ld[4][2];
+    const uint8_t* gt = qt + TILE;
     v8h p[2], ds[2], gc[ACC], qc[ACC];
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) ld[r][e] = *US_LDS_AT(const v4f, st + (qb * 32 + 8 * r + 4 * half) * 8 + 16 * e);
     products(nt, nqb, next);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const v4f x = ld[r / 4][r % 4 / 2];
-      cur.s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(cur.s[r], a.c2, -x[r % 2 * 2]));
-      cur.dp[r] = cur.s[r] * (cur.dp[r] - x[r % 2 * 2 + 1]);
+      cur.s[r] = __builtin_amdgcn_exp2f(cur.s[r] * a.c2);
+      cur.dp[r] *= cur.s[r];
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -585,14 +578,15 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
     }
 #pragma unroll
     for (int j = 0; j < ACC; ++j) gc[j] = at.columns(gt, 2 * qb, j);
-    next_lds_reads<8 + AHEAD>();
+    next_lds_reads<1 + AHEAD>();
 #pragma unroll
     for (int i = 0; i < 4 * NB; ++i) {
       next_mfma<1>();
       next_lds_reads<1>();
       next_exp<(16 + 4 * NB - 1) / (4 * NB)>();
-      next_valu<(64 + 4 * NB - 1) / (4 * NB)>();
+      next_valu<(48 + 4 * NB - 1) / (4 * NB)>();
     }
+    next_mfma<2>();
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -734,16 +728,13 @@ Cut dq_cut(const CrossCall& c) { return fwd_cut(c); }
 // heads' distances (us: batch 4, 24 heads by 8 key heads of 80, 2 queries over 12283 keys 72 -> 28; 8 by 4 of 96, 644 queries, 22 tiles or 21: 59 or 62).
 struct QueryTiles {
   bool across;
-  long tiles;              // of a key head
-  long per_head, per_kv;   // rows of `rows`
+  long tiles;      // of a key head
 };
 QueryTiles query_tiles(const CrossCall& c, int bq) {
   const long rep = c.heads / c.kv_heads, own = rep * ceil_div(c.sq, bq), all = ceil_div(rep * c.sq, bq);
   const long most = c.lq.head > c.lo.head ? c.lq.head : c.lo.head, row = c.lq.row > c.lo.row ? c.lq.row : c.lo.row;
   const bool fits = 2 * ((rep - 1) * most + c.sq * row) < (1l << 30);
-  if (8 * all <= 7 * own && fits) return {true, all, 0, (rep * c.sq + 31) / 32 * 32};      // (whole lines)
-  const long per = (c.sq + 31) / 32 * 32;
-  return {false, own, per, rep * per};
+  return 8 * all <= 7 * own && fits ? QueryTiles{true, all} : QueryTiles{false, own};
 }
 Cut dkv_cut(const CrossCall& c) {
   return with_blocks(c.dh, [&](auto nb) {
@@ -753,8 +744,7 @@ Cut dkv_cut(const CrossCall& c) {
 }
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-// (the larger of both ways, which the layouts choose from)
-size_t rows_bytes(const CrossCall& c) { return up256((size_t)c.batch * c.heads * ((c.sq + 31) / 32 * 32) * 8); }
+size_t rows_bytes(const CrossCall& c) { return up256((size_t)c.batch * c.heads * ((c.sq + 31) / 32 * 32) * 16); }
 
 template <class K>
 hipError_t launch(K kernel, FuncConfig& config, int lds, const AttendArgs& a, hipStream_t st) {
@@ -815,13 +805,10 @@ hipError_t launch_cross_fwd(const CrossCall& c, void* workspace, hipStream_t st)
 hipError_t launch_cross_bwd(const CrossCall& c, void* dQ, void* dK, void* dV, float beta_q, float beta_kv, void* workspace, hipStream_t st) {
   const int xcds = device_info().xcds;
   AttendArgs a = cross_args(c);
-  a.rows = (float2*)workspace;
+  a.rows = (v4i*)workspace;
   a.part = (float*)((uint8_t*)workspace + rows_bytes(c));
   a.lse = c.lse;
   const QueryTiles qt = with_blocks(c.dh, [&](auto nb) { return query_tiles(c, DkvCfg<decltype(nb)::value>::BQ); });
-  a.across = qt.across;
-  a.rows_per_head = (int)qt.per_head;
-  a.rows_per_kv = (int)qt.per_kv;
   if (c.sq > 0) {
     AttendArgs q = a;
     q.out = (_Float16*)dQ;

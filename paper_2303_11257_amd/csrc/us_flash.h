@@ -129,6 +129,27 @@ __device__ __forceinline__ v16f zero16() {
 }
 __device__ __forceinline__ v16f mfma32(v8h a, v8h b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
+// What dK and dV need of a query row, L / c2 and D (below, us_cross.hip), as an operand of one more product: -x as the sum of three BF16 values, exactly, each
+// of 8 bits.  In slots 0 .. 2 and 3 .. 5 of the sixteen that the product adds up, against ones there and zeros elsewhere (row_ones).
+__device__ __forceinline__ v4i row_stat(float x, float y) {
+  auto part = [](float& v) {      // takes its highest 8 bits off
+    const uint32_t top = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
+    v -= __builtin_bit_cast(float, top);
+    return top;
+  };
+  x = -x;
+  y = -y;
+  const uint32_t x0 = part(x), x1 = part(x), x2 = part(x), y0 = part(y), y1 = part(y), y2 = part(y);
+  return v4i{(int)(x0 >> 16 | x1), (int)(x2 >> 16 | y0), (int)(y1 >> 16 | y2), 0};
+}
+__device__ __forceinline__ v4i row_ones(bool second, int half) {
+  return half ? v4i{0, 0, 0, 0} : second ? v4i{0, 0x3f800000, 0x3f803f80, 0} : v4i{0x3f803f80, 0x00003f80, 0, 0};
+}
+__device__ __forceinline__ v16f mfma32_bf16(v4i a, v4i b, v16f c) {
+  typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
+
 // eight of a lane's sixteen results, rounded: the operand of the next product (t: which eight)
 __device__ __forceinline__ v8h round8(const v16f& x, int t) {
   v8h h;
@@ -245,21 +266,13 @@ struct AttendArgs {
   _Float16 *out, *dk, *dv;  // O or dQ (out_batch ..), dK and dV (laid out as k)
   long out_batch, out_head, out_row;
   float* lse;               // forward: L, or NULL
-  float2* rows;             // backward: {log2(e) L - log2(a), D} of [batch * kv][rows_per_kv]
+  v4i* rows;                // backward: RowStat of every query row, [batch * heads][sq]
   float* part;              // parts of split sums
   float2* stats;            // forward: {largest score (base 2), sum} of a part's rows
   long part_stride;         // elements between parts
   Items items;
   FastDiv by_sq;
   int batch, heads, kv, rep, sq, sk, dh, splits, per_split, tiles;      // tiles: of 16 rows (us_paged.hip)
-  // backward: rows of `rows` per key head; whether a tile of queries goes on in the next head; a head's rows in `rows` where it does not
-  int rows_per_kv, rows_per_head;
-  bool across;
-  // the row of `rows` of query q of the h-th head of a key head; across: of row q of the key head
-  template <bool ACROSS>
-  __device__ __forceinline__ long row_at(int b, int kvh, int h, int q) const {
-    return ((long)b * kv + kvh) * rows_per_kv + (ACROSS ? q : h * rows_per_head + q);
-  }
   float c2, alpha, beta;    // c2 = dh^-1/2 log2(e);  alpha <= 0: n^1/2;  beta: factor of the gradient's store
   // The item with the slot-th most keys, of up to 64, which the lanes rank against one another: the longest first, so that the CUs' shares come out even (us: 16 items
   // of 16 heads of 64, 512 queries, 64 to 1024 keys: forward 35 -> 31, dQ 50 -> 44.  dK and dV, whose workgroups have equal work or none, do without: 70 or 75).
