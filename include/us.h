@@ -505,8 +505,8 @@ us_status us_keep8_load(const void* codes, const void* scales, void* X, long ld,
  * of the weights' gradients, added in a fixed order; it is needed whether or not they are asked for.  Without tokens nothing is written.  Outputs must
  * not overlap inputs or one another.
  *
- * us_attention_* then wants s a multiple of 16, the same s for queries and keys, and takes no mask: one token of generation, an odd s and a causal
- * layer go on to the caller's own attention.  The projection's gradients: with shared heads dQKV's key and value columns carry (heads / kv_heads)^-1/2,
+ * us_attention_* then wants s a multiple of 16, the same s for queries and keys, and takes no mask; us_attention_cross_* takes any s, and keys that end early;
+ * one token of generation goes on to us_cache_store and us_attention_paged; a causal layer to the caller's own attention.  The projection's gradients: with shared heads dQKV's key and value columns carry (heads / kv_heads)^-1/2,
  * which a weight's gradient may (it is a cut-edge, column by column) and the projection's input gradient, which adds all columns, may not (Sec. 5.2 step 2):
  * for a multiple of the loss's gradient give dQ the same factor first (us_weighted_add(dQ, dQ, dQ, n, US_F16, c, 0)).
  */
@@ -578,6 +578,7 @@ size_t us_attention_cross_workspace_bytes(long batch, long heads, long kv_heads,
  *     weights[page, key head, slot] += sum of p_i over the query heads that share the key head      (FP32, laid out as the pools' slots; may be NULL)
  *   Q: FP16 [batch, heads * dh], rows ldq elements apart (a multiple of 8); O likewise, ldo.  max_len: the host's bound on the lengths: the work is shared out for
  *   it, and longer sequences are cut off there.  Without positions O is 0.  A slot that several positions of the call share must not have weights: their additions race.
+ *   The caller clears the weights of slots that new positions take.
  *   FP32 sums; p is rounded to FP16 for the product with V.  Workspace (16-byte aligned, undefined on entry and exit): us_attention_paged_workspace_bytes, asked with
  *   the device current that runs the call.
  *
@@ -586,7 +587,8 @@ size_t us_attention_cross_workspace_bytes(long batch, long heads, long kv_heads,
  *   table_to == table: in place; the slots behind are left as they were, and a page must belong to one sequence only.  Another table_to (int32
  *   [batch, table_to_ld], pages of the same pools that hold none of the sequences): the kept rows are copied there.
  *   new_len[b] = min(len[b], keep) (int32 [batch], may be len itself, or NULL), kept: int32 [batch, kv_heads, keep], the positions that were kept, -1 behind a shorter
- *   sequence's.  0 <= recent <= keep <= 2^20.  max_len as above.
+ *   sequence's.  0 <= recent <= keep <= 2^20.  max_len as above.  A position on a page that there is not comes after all others; where it is kept all the same, no row
+ *   moves, and its new slot is left as it was.
  *
  * dh a multiple of 16 up to US_ROPE_HEAD_MAX; batch and heads up to 65535; batch * heads up to 2^22, batch * kv_heads * ceil(max_len / 256) up to 2^23 (eviction:
  * batch * kv_heads up to 2^20); a sequence's new rows, s * kv_heads * dh / 8, up to 2^31 - 1.  All pools and rows 16-byte aligned.  Results do not depend on scheduling.
