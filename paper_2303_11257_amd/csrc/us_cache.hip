@@ -186,7 +186,9 @@ __global__ void __launch_bounds__(kSelect) cache_select_kernel(Pool p, const flo
 // ---- eviction: the rows ------------------------------------------------------------------------------------------------------
 // Kept row i goes to position i.  In place a destination never lies behind its source, and sources are in order: a workgroup that takes the rows of a key
 // head in rounds, reading a whole round before it writes it, overwrites nothing that is still to be read.  A round has kUnroll rows per thread group, their
-// reads in flight together.
+// reads in flight together; in place the next round's are looked up meanwhile (us: 11 x 8 heads of 96, up to 6756 -> 2594 in FP16 72 -> 64, 64 x 8 of 128, 2000 kept
+// 193 -> 176), and there are no more threads than pieces (29 x 23 heads, 19 kept: 12 -> 5.5).  Elsewhere a workgroup has one round (16 x 8 heads of 128 codes, 4096
+// kept of up to 8192: 64; the loop around it leaves the order of its reads as it is: without it 73).
 constexpr int kUnroll = 4;
 template <bool IN_PLACE>
 __global__ void __launch_bounds__(kSelect) cache_move_kernel(Pool p, float* weights, const int* table_to, long table_to_ld, const int* len, int* new_len, const int* kept,
@@ -203,24 +205,28 @@ __global__ void __launch_bounds__(kSelect) cache_move_kernel(Pool p, float* weig
   const int r = tid / chunks, chunk = tid % chunks;
   const int first = (int)blockIdx.y * per_part, last = keep < first + per_part ? keep : first + per_part;
   uint8_t* const base = which ? p.v : p.k;
-  for (int i0 = first; i0 < last; i0 += kUnroll * rows) {
-    int pos[kUnroll];
-    long src[kUnroll], dst[kUnroll];
-    v4i x[kUnroll];
-    float w[kUnroll];
+  constexpr int U = kUnroll;
+  long src[U], dst[U];
+  // where the rows of a round come from and go to, -1: nowhere.  A round's are looked up while the rows of the one before it are on their way.
+  auto look = [&](int i0) {
+    int pos[U];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       const int i = i0 + u * rows + r;
       pos[u] = r < rows && i < last ? from[i] : -1;
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       const int i = i0 + u * rows + r;
       src[u] = pos[u] < 0 || (IN_PLACE && pos[u] == i) ? -1 : p.row_of(p.table, p.table_ld, b, head, pos[u]);
       dst[u] = src[u] < 0 ? -1 : p.row_of(table_to, table_to_ld, b, head, i);
     }
+  };
+  v4i x[U];
+  float w[U];
+  auto load = [&] {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       x[u] = v4i{0, 0, 0, 0};
       w[u] = 0.0f;
       if (dst[u] >= 0) {
@@ -228,18 +234,33 @@ __global__ void __launch_bounds__(kSelect) cache_move_kernel(Pool p, float* weig
         else w[u] = weights[src[u]];
       }
     }
-    if constexpr (IN_PLACE) {
+  };
+  auto store = [&](const long (&to)[U]) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) asm volatile("" : "+v"(x[u]), "+v"(w[u]));      // (used here: the loads have landed, not only left, when the others go on)
-      __syncthreads();
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if (dst[u] >= 0) {
-        if (which < 2) *reinterpret_cast<v4i*>(base + dst[u] * row_bytes + chunk * 16) = x[u];
-        else weights[dst[u]] = w[u];
+    for (int u = 0; u < U; ++u)
+      if (to[u] >= 0) {
+        if (which < 2) *reinterpret_cast<v4i*>(base + to[u] * row_bytes + chunk * 16) = x[u];
+        else weights[to[u]] = w[u];
       }
-    if constexpr (IN_PLACE) __syncthreads();
+  };
+  if constexpr (IN_PLACE) look(first);
+  for (int i0 = first; i0 < last; i0 += U * rows) {
+    if constexpr (IN_PLACE) {
+      load();
+      long to[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) to[u] = dst[u];
+      if (i0 + U * rows < last) look(i0 + U * rows);
+#pragma unroll
+      for (int u = 0; u < U; ++u) asm volatile("" : "+v"(x[u]), "+v"(w[u]));      // (used here: the loads have landed, not only left, when the others go on)
+      __syncthreads();
+      store(to);
+      __syncthreads();
+    } else {
+      look(i0);
+      load();
+      store(dst);
+    }
   }
 }
 __global__ void __launch_bounds__(kThreads) cache_len_kernel(int* new_len, int batch) {
@@ -294,10 +315,13 @@ hipError_t launch_cache_evict(const CacheCall& c, float* weights, const int* tab
   if (e != hipSuccess) return e;
   const int row_bytes = (int)(c.dh * (c.fp8 ? 1 : 2));
   if (in_place) {
-    cache_move_kernel<true><<<3 * groups, kSelect, 0, st>>>(p, weights, table_to, table_to_ld, len, new_len, kept, (int)max_len, (int)keep, row_bytes, (int)keep);
+    // no more threads than there are pieces for
+    const long pieces = (keep * (row_bytes / 16) + kUnroll - 1) / kUnroll;
+    const unsigned threads = pieces >= kSelect ? kSelect : (unsigned)((pieces + 63) / 64 * 64);
+    cache_move_kernel<true><<<3 * groups, threads, 0, st>>>(p, weights, table_to, table_to_ld, len, new_len, kept, (int)max_len, (int)keep, row_bytes, (int)keep);
   } else {
     // a round of a workgroup's rows each
-    const int per_part = kUnroll * kThreads * 16 / row_bytes;
+    const int per_part = kUnroll * (kThreads / (row_bytes / 16));
     cache_move_kernel<false><<<dim3(3 * groups, (unsigned)((keep + per_part - 1) / per_part)), kThreads, 0, st>>>(p, weights, table_to, table_to_ld, len, new_len, kept,
                                                                                                               (int)max_len, (int)keep, row_bytes, per_part);
   }

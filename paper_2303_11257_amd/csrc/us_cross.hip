@@ -66,7 +66,9 @@ struct RowsOf {
 // ---- forward -----------------------------------------------------------------------------------------------------------
 template <int NB>
 struct FwdCfg {
-  static constexpr int BK = NB <= 4 ? 64 : 32, STAGES = 2;
+  // (two blocks of 32 keys at a time, so that a product need not wait for the one before it; above 128 columns as well: 64 heads of 192, 1024 x 1024, 103 -> 97 us, ragged
+  // batches of 256 columns 172 -> 160 and 264 -> 234)
+  static constexpr int BK = 64, STAGES = 2;
   static constexpr int TILE = BK * RowTile<NB>::P, LDS = STAGES * 2 * TILE;
 };
 
@@ -708,7 +710,8 @@ AttendArgs cross_args(const CrossCall& c) {
 
 long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
-// How a reduction of `steps` tiles is cut so that `items` workgroups become enough for the device.
+// How a reduction of `steps` tiles is cut so that `items` workgroups become enough for the device: two per CU (us of the forward pass with 2, 3, 4, 6: 8 + 8 heads of 128,
+// 512 x 4096 32, 38, 62, 65; 42 heads of 128 over ragged 9000 keys 52, 62, 72, 70; 64 heads of 64, ragged 8192 58, 57, 60, 63).
 struct Cut {
   int splits;
   long per;       // steps of a part
