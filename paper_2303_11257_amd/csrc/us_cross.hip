@@ -470,6 +470,8 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 4 : NB <= 4 ? 2 : 1) cross
 // ---- backward: dK and dV ------------------------------------------------------------------------------------------------------
 // A wave takes 32 keys, whose fragments and gradients stay in registers, and all queries of the heads that share them, tile by tile through LDS.
 // Heads above 128 columns are accumulated in two halves by two workgroups, whose products with all columns are made twice: 512 registers hold no more.
+// Up to 96 columns two waves a SIMD (us, 16 x 16 heads of 96, 512 queries over up to 1024 keys: one wave with four fragments read ahead 128, two with two 82; of the rows across
+// heads only one fragment more fits the registers).
 template <int NB>
 struct DkvCfg {
   static constexpr int HALVES = NB > 4 ? 2 : 1, ACC = NB / HALVES;
@@ -480,9 +482,9 @@ struct DkvBlock {
   v16f s, dp;
 };
 template <int NB, bool ACROSS>
-__global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, NB <= 3 ? 2 : 1) cross_dkv_kernel(AttendArgs a) {
   using C = DkvCfg<NB>;
-  constexpr int BQ = C::BQ, QB = BQ / 32, TILE = C::TILE, ACC = C::ACC, AHEAD = kAhead<NB>;
+  constexpr int BQ = C::BQ, QB = BQ / 32, TILE = C::TILE, ACC = C::ACC, AHEAD = NB == 3 ? (ACROSS ? 1 : 2) : kAhead<NB>;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -490,8 +492,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
   if (it.b < 0) return;
   const int b = it.b, kvh = it.kvh, tile = it.y, split = it.z, first = it.x * ACC;
   const int n = a.keys_of(b);
-  const int key = tile * kRows + wave * 32 + l32;
-  const bool on = key < a.sk;
+  const int row0 = tile * kRows + wave * 32;      // of the wave's keys
   // the tiles of the sharing heads' queries, one head after the other, each with tiles of its own or all in the same ones (across); a split takes per_split of them
   const int nrows = a.rep * a.sq, qtiles = ACROSS ? (nrows + BQ - 1) / BQ : (a.sq + BQ - 1) / BQ, total = ACROSS ? qtiles : a.rep * qtiles;
   const int begin = split * a.per_split;
@@ -502,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
   if (begin >= end && a.splits == 1) {      // zeros, without the detour through LDS (the same: 73 -> 70 us)
 #pragma unroll
     for (int i = 0; i < 2 * ACC; ++i) {
-      const int c = i * 64 + lane, row = c / (4 * ACC), col = 32 * first + 8 * (c - row * (4 * ACC)), r = tile * kRows + wave * 32 + row;
+      const int c = i * 64 + lane, row = c / (4 * ACC), col = 32 * first + 8 * (c - row * (4 * ACC)), r = row0 + row;
       if (r < a.sk && col < a.dh) {
         wt_store(reinterpret_cast<v4i*>(dk_rows(r) + col), v4i{});
         wt_store(reinterpret_cast<v4i*>(dv_rows(r) + col), v4i{});
@@ -531,13 +532,16 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
       lg.request((const uint8_t*)G + (long)q0 * a.g.row, a.sq - q0, a.g.row, a.dh, to + TILE, wave);
     }
     const int left = (ACROSS ? nrows : a.sq) - q0;      // (zeros behind them, as Q and dO are there: P is then 1, and all that it meets 0)
-    if (wave == 0) load_to_lds(buffer_words(a.rows + ((long)b * a.heads + head) * a.sq + q0, (left < BQ ? left : BQ) * 16), to + 2 * TILE, (uint32_t)lane * 16);
+    if (wave == 0) load_to_lds(buffer_words(a.rows + ((long)b * a.heads + head) * a.sq + q0, (left < BQ ? left : BQ) * 16), to + 2 * TILE, threadIdx.x * 16);
     if (++rtile == qtiles) { rtile = 0; ++rhead; }
   };
   if (begin < end) request(0);
   v8h kf[2 * NB], vf[2 * NB];
-  load_fragments<NB>(kf, (const _Float16*)((const uint8_t*)(a.k.p + b * a.k.batch + kvh * a.k.head) + (long)key * a.k.row), key < n, a.dh, half);
-  load_fragments<NB>(vf, (const _Float16*)((const uint8_t*)(a.v.p + b * a.v.batch + kvh * a.v.head) + (long)key * a.v.row), key < n, a.dh, half);
+  {
+    const int key = row0 + l32;
+    load_fragments<NB>(kf, (const _Float16*)((const uint8_t*)(a.k.p + b * a.k.batch + kvh * a.k.head) + (long)key * a.k.row), key < n, a.dh, half);
+    load_fragments<NB>(vf, (const _Float16*)((const uint8_t*)(a.v.p + b * a.v.batch + kvh * a.v.head) + (long)key * a.v.row), key < n, a.dh, half);
+  }
   TileReads<NB, ACC> at;
   at.init(lane, first);
   v16f dk[ACC], dv[ACC];
@@ -634,6 +638,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
     }
   }
   const float c = a.c2 * kLn2F;
+  const int key = NB == 3 ? row_again(row0) : row0 + l32;      // (three blocks have not one register to spare)
 #pragma unroll
   for (int j = 0; j < ACC; ++j) {
     if (key >= n) dk[j] = dv[j] = zero16();
@@ -641,15 +646,17 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 2 : 1) cross_dkv_kernel(At
   }
   if (a.splits > 1) {
     float* out = a.part + split * a.part_stride + (((long)b * a.kv + kvh) * a.sk + key) * 2 * a.dh;
+    const bool on = key < a.sk;
+    const int half_again = lane_again() >> 5;
 #pragma unroll
     for (int j = 0; j < ACC; ++j) {
-      store_block_f32(out, 32 * (first + j), a.dh, on, half, dk[j], c);
-      store_block_f32(out + a.dh, 32 * (first + j), a.dh, on, half, dv[j], 1.0f);
+      store_block_f32(out, 32 * (first + j), a.dh, on, half_again, dk[j], c);
+      store_block_f32(out + a.dh, 32 * (first + j), a.dh, on, half_again, dv[j], 1.0f);
     }
     return;
   }
-  store_rows<ACC>(lds, dk, c * a.beta, tile * kRows + wave * 32, dk_rows, a.dh, 32 * first, lane, wave);
-  store_rows<ACC>(lds, dv, a.beta, tile * kRows + wave * 32, dv_rows, a.dh, 32 * first, lane, wave);
+  store_rows<ACC>(lds, dk, c * a.beta, row0, dk_rows, a.dh, 32 * first, lane_again(), wave);
+  store_rows<ACC>(lds, dv, a.beta, row0, dv_rows, a.dh, 32 * first, lane_again(), wave);
 }
 
 // Sums of split gradients, part after part: `rows` rows of dh columns `row_stride` elements apart in a part; row = (batch * heads + head) * s + t.

@@ -25,16 +25,16 @@ __device__ __forceinline__ float halves_sum(float v) {
 }
 
 // ---- tiles of rows in LDS ---------------------------------------------------------------------------------------------
-// A row of up to 32 NB halves takes `pitch` bytes, a power of two; its 16-byte chunk c lies at c ^ swz(row).  The bits are chosen for both
-// ways of reading: sixteen lanes that read the same chunk of rows r .. r + 15, and a transposing read whose 32 lanes touch 64 bytes in each of
-// four rows; both meet every bank once.
+// A row of up to 32 NB halves takes P bytes; its 16-byte chunk c lies at c ^ swz(row).  The bits are chosen for both ways of reading: sixteen lanes that read the same
+// chunk of rows r .. r + 15, and a transposing read whose 32 lanes touch 64 bytes in each of four rows; both meet every bank once.  Where P is no multiple of the
+// banks' 256 bytes the rows themselves start on other banks: 192 moves each by three quarters, 384 by a half, as 64 and 128 do by one quarter and a half.
 template <int NB>
 struct RowTile {
-  static constexpr int P = NB == 1 ? 64 : NB == 2 ? 128 : NB <= 4 ? 256 : 512;
-  static constexpr int CHUNKS = P / 16;
+  static constexpr int P = 64 * NB;
+  static_assert(NB <= 4 || NB == 6 || NB == 8, "");
   __device__ __forceinline__ static int swz(int row) {
-    if (P == 64) return (row >> 2) & 3;
-    if (P == 128) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+    if (P % 128) return (row >> 2) & 3;
+    if (P % 256) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
     return ((row & 3) << 2) | ((row >> 2) & 3);
   }
 };

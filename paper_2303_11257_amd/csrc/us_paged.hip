@@ -54,8 +54,8 @@ struct ValueTile {
       if (P == 128) return ((row >> 1) & 3) | ((row >> 4) & 1) << 2;
       return (row & 7) | ((row >> 4) & 1) << 3;
     }
-    if (P == 64) return ((row >> 2) & 1) << 1;
-    if (P == 128) return ((row >> 1) & 3) << 1;
+    if (P % 128) return ((row >> 2) & 1) << 1;
+    if (P % 256) return ((row >> 1) & 3) << 1;
     return (row & 7) << 1;
   }
 };
