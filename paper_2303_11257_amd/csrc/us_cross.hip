@@ -295,7 +295,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows,
 // keys D is therefore the sum of p dO v itself, from products made twice (2-norm error of dQ, unit normal inputs, 5 to 120 keys: 2.95e-4 to 2.98e-4, two roundings to FP16; of 140 to 400 keys, from O,
 // 3.2e-4 to 3.1e-4).
 constexpr int kFewKeys = 128;
-// Heads of up to 64 columns: 124 registers a lane, so four waves a SIMD.
+// Heads of up to 64 columns: 124 registers a lane, so four waves a SIMD.  Of up to 96: three, with fewer fragments read ahead (us: 4 x 32 heads by 8 of 96, 2048 x 2048 370 ->
+// 339, 59 x 6 by 3, 470 x 547 70 -> 65; where a SIMD has one wave it loses half a microsecond of 10).
 // Where a tile is one block of keys (dh > 128) three of them are on their way at a time (us: 32 heads of 256, ragged batch of 5, 869 x 528: 166 -> 156; 130 x 1030:
 // 36 -> 33; the forward pass gains nothing by it: 112 -> 117, 26 -> 26).  Requests then go on behind the last tile, for zeros: every wave has as many loads on its way.
 template <int NB>
@@ -303,7 +304,7 @@ struct DqCfg {
   static constexpr int BK = NB <= 4 ? 64 : 32, STAGES = NB <= 4 ? 2 : 4, TILE = BK * RowTile<NB>::P, LDS = STAGES * 2 * TILE;
 };
 template <int NB>
-__global__ void __launch_bounds__(kThreads, NB <= 2 ? 4 : NB <= 4 ? 2 : 1) cross_dq_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, NB <= 2 ? 4 : NB == 3 ? 3 : NB <= 4 ? 2 : 1) cross_dq_kernel(AttendArgs a) {
   using C = DqCfg<NB>;
   constexpr int BK = C::BK, KB = BK / 32, TILE = C::TILE;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 4 : NB <= 4 ? 2 : 1) cross
   }
   TileReads<NB> at;
   at.init(lane);
-  constexpr int AHEAD = kAhead<NB>, CA = NB <= 4 ? NB : 4;
+  constexpr int AHEAD = NB == 3 ? 3 : kAhead<NB>, CA = NB == 3 ? 1 : NB <= 4 ? NB : 4;
   // raw scores and dO v of 32 keys, in turn: a product that adds to the one just before it has to wait for it
   auto products = [&](const uint8_t* kt, int kb, v16f& s, v16f& dp) {
     auto fragment = [&](int i) { return at.rows(i % 2 ? kt + TILE : kt, kb, i / 2); };
