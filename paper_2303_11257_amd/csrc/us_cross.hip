@@ -718,22 +718,35 @@ AttendArgs cross_args(const CrossCall& c) {
 
 long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
-// How a reduction of `steps` tiles is cut so that `items` workgroups become enough for the device: two per CU (us of the forward pass with 2, 3, 4, 6: 8 + 8 heads of 128,
-// 512 x 4096 32, 38, 62, 65; 42 heads of 128 over ragged 9000 keys 52, 62, 72, 70; 64 heads of 64, ragged 8192 58, 57, 60, 63).
+// How a reduction of `steps` tiles is cut into parts of at least `least`: the fewest steps one after the other, where a CU holds `per_cu` of the workgroups at once, each
+// starts and ends in the time of `fixed` steps, and parts are added in that of four; none where that saves less than an eighth.  Only the most parts that fit one to four
+// rounds are looked at.  (us, against parts for two workgroups per CU whatever runs at once: 12 heads of 128, 829 x 912, both directions 102 -> 88; 12 by 6, 370 x 2505 120 -> 97;
+// 56 by 14 heads of 96, 75 x 519 58 -> 55.  The forward pass with parts for 2, 3, 4 and 6 workgroups per CU, where two run: 16 heads of 128, 512 x 4096 32, 38, 62, 65; 42 over
+// ragged 9000 keys 52, 62, 72, 70; of 64 columns, where four run, 64 over ragged 8192 keys 58, 57, 60, 63.)
 struct Cut {
   int splits;
   long per;       // steps of a part
 };
-Cut cut(long items, long steps, long least) {
-  const long want = 2l * device_info().cus;
-  long splits = items >= want || items < 1 ? 1 : want / items;
-  if (splits > steps / least) splits = steps / least;
-  if (splits < 1) splits = 1;
-  const long per = steps > 0 ? ceil_div(steps, splits) : 1;
-  return {steps > 0 ? (int)ceil_div(steps, per) : 1, per};
+Cut cut(long items, long steps, long least, long per_cu, long fixed) {
+  if (items < 1 || steps < 1) return {1, steps > 0 ? steps : 1};
+  const long slots = per_cu * device_info().cus;
+  Cut best{1, steps};
+  long least_cost = ceil_div(items, slots) * (steps + fixed) * 7 / 8;
+  for (long rounds = 1; rounds <= 4; ++rounds) {
+    long splits = rounds * slots / items;
+    if (splits > steps / least) splits = steps / least;
+    if (splits < 2) continue;
+    const long per = ceil_div(steps, splits), parts = ceil_div(steps, per), cost = ceil_div(items * parts, slots) * (per + fixed) + 4;
+    if (cost < least_cost) {
+      least_cost = cost;
+      best = {(int)parts, per};
+    }
+  }
+  return best;
 }
 long row_tiles(const CrossCall& c) { return ceil_div(c.heads / c.kv_heads * c.sq, kRows); }
-Cut fwd_cut(const CrossCall& c) { return cut(c.batch * c.kv_heads * row_tiles(c), ceil_div(c.sk, 64), 4); }
+// (two waves on a SIMD are as fast as three or four)
+Cut fwd_cut(const CrossCall& c) { return cut(c.batch * c.kv_heads * row_tiles(c), ceil_div(c.sk, 64), 4, c.dh <= 128 ? 2 : 1, 3); }
 Cut dq_cut(const CrossCall& c) { return fwd_cut(c); }
 // How dK's and dV's workgroups take the queries: tiles of each head, or of all heads that share a key head, where that makes fewer tiles and 31 bits hold the
 // heads' distances (us: batch 4, 24 heads by 8 key heads of 80, 2 queries over 12283 keys 72 -> 28; 8 by 4 of 96, 644 queries, 22 tiles or 21: 59 or 62).
@@ -750,7 +763,7 @@ QueryTiles query_tiles(const CrossCall& c, int bq) {
 Cut dkv_cut(const CrossCall& c) {
   return with_blocks(c.dh, [&](auto nb) {
     using C = DkvCfg<decltype(nb)::value>;
-    return cut(C::HALVES * c.batch * c.kv_heads * ceil_div(c.sk, kRows), query_tiles(c, C::BQ).tiles, 256 / C::BQ);
+    return cut(C::HALVES * c.batch * c.kv_heads * ceil_div(c.sk, kRows), query_tiles(c, C::BQ).tiles, 256 / C::BQ, c.dh <= 96 ? 2 : 1, 384 / C::BQ);
   });
 }
 
