@@ -754,16 +754,22 @@ struct QueryTiles {
   bool across;
   long tiles;      // of a key head
 };
-QueryTiles query_tiles(const CrossCall& c, int bq) {
+QueryTiles query_tiles(const CrossCall& c, int bq, bool near) {
   const long rep = c.heads / c.kv_heads, own = rep * ceil_div(c.sq, bq), all = ceil_div(rep * c.sq, bq);
-  const long most = c.lq.head > c.lo.head ? c.lq.head : c.lo.head, row = c.lq.row > c.lo.row ? c.lq.row : c.lo.row;
-  const bool fits = 2 * ((rep - 1) * most + c.sq * row) < (1l << 30);
-  return 8 * all <= 7 * own && fits ? QueryTiles{true, all} : QueryTiles{false, own};
+  return 8 * all <= 7 * own && near ? QueryTiles{true, all} : QueryTiles{false, own};
 }
+bool heads_near(const CrossCall& c) {
+  const long most = c.lq.head > c.lo.head ? c.lq.head : c.lo.head, row = c.lq.row > c.lo.row ? c.lq.row : c.lo.row;
+  return most < (1l << 30) && 2 * ((c.heads / c.kv_heads - 1) * most + c.sq * row) < (1l << 30);
+}
+// (As many parts whatever the layouts, which the workspace's size is not asked with.)
 Cut dkv_cut(const CrossCall& c) {
   return with_blocks(c.dh, [&](auto nb) {
     using C = DkvCfg<decltype(nb)::value>;
-    return cut(C::HALVES * c.batch * c.kv_heads * ceil_div(c.sk, kRows), query_tiles(c, C::BQ).tiles, 256 / C::BQ, c.dh <= 96 ? 2 : 1, 384 / C::BQ);
+    Cut s = cut(C::HALVES * c.batch * c.kv_heads * ceil_div(c.sk, kRows), query_tiles(c, C::BQ, true).tiles, 256 / C::BQ, c.dh <= 96 ? 2 : 1, 384 / C::BQ);
+    const long tiles = query_tiles(c, C::BQ, heads_near(c)).tiles;
+    if (tiles > 0) s.per = ceil_div(tiles, s.splits), s.splits = (int)ceil_div(tiles, s.per);
+    return s;
   });
 }
 
@@ -786,7 +792,9 @@ size_t cross_fwd_workspace_bytes(const CrossCall& c) {
   return s.splits == 1 ? 0 : up256(s.splits * rows * 8) + s.splits * rows * c.dh * 4;
 }
 size_t cross_bwd_workspace_bytes(const CrossCall& c) {
-  const Cut q = dq_cut(c), k = dkv_cut(c);
+  CrossCall near = c;
+  near.lq = near.lo = us_heads_layout{};
+  const Cut q = dq_cut(c), k = dkv_cut(near);
   const size_t nq = q.splits == 1 ? 0 : (size_t)q.splits * c.batch * c.heads * c.sq * c.dh * 4;
   const size_t nk = k.splits == 1 ? 0 : (size_t)k.splits * c.batch * c.kv_heads * c.sk * c.dh * 8;
   return rows_bytes(c) + (nq > nk ? nq : nk);
@@ -832,7 +840,7 @@ hipError_t launch_cross_bwd(const CrossCall& c, void* dQ, void* dK, void* dV, fl
   a.rows = (v4i*)workspace;
   a.part = (float*)((uint8_t*)workspace + rows_bytes(c));
   a.lse = c.lse;
-  const QueryTiles qt = with_blocks(c.dh, [&](auto nb) { return query_tiles(c, DkvCfg<decltype(nb)::value>::BQ); });
+  const QueryTiles qt = with_blocks(c.dh, [&](auto nb) { return query_tiles(c, DkvCfg<decltype(nb)::value>::BQ, heads_near(c)); });
   if (c.sq > 0) {
     AttendArgs q = a;
     q.out = (_Float16*)dQ;

@@ -190,6 +190,29 @@ def test_heads_that_share_keys_also_share_tiles(dims, layout):
     c.check(what=f"{layout} ")
 
 
+def test_heads_too_far_apart_to_share_tiles():
+    """Shared key heads whose query heads lie more than 31 bits apart: the workspace that is asked for, without layouts, serves this call too."""
+    heads, sq, sk, dh, far = 64, 2, 128, 64, (1 << 23) + 8
+    near = Call(1, heads, 1, sq, sk, dh, seed=12)
+    near.fwd()
+    near.bwd()
+    size = far * (heads - 1) + sq * dh
+    lay = us.HeadsLayout(size, far, dh)
+    Q, O, G, dQ = (torch.empty(size, dtype=F, device=DEV) for _ in range(4))
+    at = lambda t: t.as_strided((heads, sq, dh), (far, dh, 1))      # noqa: E731
+    at(Q).copy_(near.Q[0]), at(G).copy_(near.G[0])
+    K, V = near.t["K"], near.t["V"]
+    dK, dV = torch.empty(sk * dh, dtype=F, device=DEV), torch.empty(sk * dh, dtype=F, device=DEV)
+    lse = torch.empty(heads * sq, dtype=torch.float32, device=DEV)
+    wsb = us.attention_cross_workspace_bytes(1, heads, 1, sq, sk, dh)
+    ws = torch.empty(wsb, dtype=torch.uint8, device=DEV)
+    us.attention_cross_fwd(ptr(Q), ptr(K), ptr(V), None, ptr(O), ptr(lse), 1, heads, 1, sq, sk, dh, 0.0, lay, None, lay, ptr(ws), wsb, stream())
+    us.attention_cross_bwd(ptr(Q), ptr(K), ptr(V), None, ptr(O), ptr(lse), ptr(G), ptr(dQ), ptr(dK), ptr(dV), 1, heads, 1, sq, sk, dh, 0.0, 0.0, 0.0, lay, None, lay, ptr(ws), wsb, stream())
+    want = near.reference(True)
+    for name, got in (("O", at(O)[None]), ("dQ", at(dQ)[None]), ("dK", dK.view(1, 1, sk, dh)), ("dV", dV.view(1, 1, sk, dh))):
+        R.close(got, want[name], name)
+
+
 def test_a_bad_query_beside_other_heads_in_its_tile():
     c = Call(1, 8, 2, 20, 150, 64, seed=6)
     c.Q[0, 5, 13, 5] = float("nan")
