@@ -485,6 +485,9 @@ struct DkvBlock {
 template <int NB, bool ACROSS>
 __global__ void __launch_bounds__(kThreads, NB <= 3 ? 2 : 1) cross_dkv_kernel(AttendArgs a) {
   using C = DkvCfg<NB>;
+  // one wave a SIMD has registers for column fragments that are read further ahead (us: 2 x 32 by 8 heads of 128, 4096 over 8192, 2690 -> 2480; 64 heads of 192 and of 256, 1024 x
+  // 1024, 219 -> 202 and 277 -> 250; eight row fragments instead of four 2600)
+  constexpr bool FAR = NB > 3;
   constexpr int BQ = C::BQ, QB = BQ / 32, TILE = C::TILE, ACC = C::ACC, AHEAD = NB == 3 ? (ACROSS ? 1 : 2) : kAhead<NB>;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
@@ -570,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 3 ? 2 : 1) cross_dkv_kernel(At
   // Block qb of the tile at qt becomes part of the gradients; meanwhile block nqb of the tile at nt is made, so that matrix core and vector ALU both have work.
   auto block = [&](DkvBlock& cur, const uint8_t* qt, int qb, DkvBlock& next, const uint8_t* nt, int nqb) {
     const uint8_t* gt = qt + TILE;
-    v8h p[2], ds[2], gc[ACC], qc[ACC];
+    v8h p[2], ds[2], gc[FAR ? 2 : 1][ACC], qc[FAR ? 2 : 1][ACC];
     __builtin_amdgcn_sched_barrier(0);
     products(nt, nqb, next);
 #pragma unroll
@@ -584,12 +587,16 @@ __global__ void __launch_bounds__(kThreads, NB <= 3 ? 2 : 1) cross_dkv_kernel(At
       ds[t] = round8(cur.dp, t);
     }
 #pragma unroll
-    for (int j = 0; j < ACC; ++j) gc[j] = at.columns(gt, 2 * qb, j);
+    for (int j = 0; j < ACC; ++j) gc[0][j] = at.columns(gt, 2 * qb, j);
+    if constexpr (FAR) {
+#pragma unroll
+      for (int j = 0; j < ACC; ++j) qc[0][j] = at.columns(qt, 2 * qb, j);
+    }
     next_lds_reads<1 + AHEAD>();
 #pragma unroll
     for (int i = 0; i < 4 * NB; ++i) {
       next_mfma<1>();
-      next_lds_reads<1>();
+      next_lds_reads<FAR ? 2 : 1>();
       next_exp<(16 + 4 * NB - 1) / (4 * NB)>();
       next_valu<(48 + 4 * NB - 1) / (4 * NB)>();
     }
@@ -597,23 +604,28 @@ __global__ void __launch_bounds__(kThreads, NB <= 3 ? 2 : 1) cross_dkv_kernel(At
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
+      const int here = FAR ? t : 0;
 #pragma unroll
       for (int j = 0; j < ACC; ++j) {
-        dv[j] = mfma32(gc[j], p[t], dv[j]);
-        qc[j] = at.columns(qt, 2 * qb + t, j);
+        dv[j] = mfma32(gc[here][j], p[t], dv[j]);
+        if (!FAR) qc[0][j] = at.columns(qt, 2 * qb + t, j);
+        else if (t == 0) gc[FAR][j] = at.columns(gt, 2 * qb + 1, j);
       }
 #pragma unroll
       for (int j = 0; j < ACC; ++j) {
-        dk[j] = mfma32(qc[j], ds[t], dk[j]);
-        if (t == 0) gc[j] = at.columns(gt, 2 * qb + 1, j);
+        dk[j] = mfma32(qc[here][j], ds[t], dk[j]);
+        if (t == 0) {
+          if (FAR) qc[FAR][j] = at.columns(qt, 2 * qb + 1, j);
+          else gc[0][j] = at.columns(gt, 2 * qb + 1, j);
+        }
       }
     }
 #pragma unroll
-    for (int t = 0; t < 3 * ACC; ++t) {
+    for (int t = 0; t < (FAR ? 2 : 3) * ACC; ++t) {
       next_mfma<1>();
       next_lds_reads<2>();
     }
-    next_mfma<ACC>();
+    next_mfma<(FAR ? 2 : 1) * ACC>();
     __builtin_amdgcn_sched_barrier(0);
   };
   // A tile's last block is needed while the next tile's first one is made, and the tile behind that is on its way: three buffers.  Behind the last tile a block is
