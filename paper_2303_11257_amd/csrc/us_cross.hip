@@ -485,9 +485,9 @@ struct DkvBlock {
 template <int NB, bool ACROSS>
 __global__ void __launch_bounds__(kThreads, NB <= 3 ? 2 : 1) cross_dkv_kernel(AttendArgs a) {
   using C = DkvCfg<NB>;
-  // one wave a SIMD has registers for column fragments that are read further ahead (us: 2 x 32 by 8 heads of 128, 4096 over 8192, 2690 -> 2480; 64 heads of 192 and of 256, 1024 x
-  // 1024, 219 -> 202 and 277 -> 250; eight row fragments instead of four 2600)
-  constexpr bool FAR = NB > 3;
+  // Column fragments are read further ahead where registers are left (us: 2 x 32 by 8 heads of 128, 4096 over 8192, 2690 -> 2480; 64 heads of 192 and of 256, 1024 x 1024,
+  // 219 -> 202 and 277 -> 250; 16 x 16 heads of 32 41 -> 39.4; eight row fragments instead of four 2600 at the first)
+  constexpr bool FAR = NB != 3;
   constexpr int BQ = C::BQ, QB = BQ / 32, TILE = C::TILE, ACC = C::ACC, AHEAD = NB == 3 ? (ACROSS ? 1 : 2) : kAhead<NB>;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
