@@ -72,6 +72,10 @@ CASES += [(lambda n=n: paged(**{n: 18}), ALIGN) for n in ("table", "len", "W")] 
 CASES += [(lambda n=n: evict(**{n: None}), NULL) for n in ("kc", "vc", "W", "table", "to", "len", "kept")] + [(lambda n=n: evict(**{n: 24}), ALIGN) for n in ("kc", "vc")]
 CASES += [(lambda n=n: evict(**{n: 18}), ALIGN) for n in ("W", "table", "to", "len", "new", "kept")]
 
+# what one launch cannot hold: 2^22 tiles of rows, 2^23 pieces of 256 positions, 2^20 key heads to choose for
+CASES += [(lambda k=k: f(batch=65535, kv=1, **k), SHAPE) for k in (dict(heads=65, sq=1), dict(heads=1, sq=8200), dict(heads=1, sq=1, sk=8200)) for f in (fwd, bwd)]
+CASES += [(lambda: paged(batch=65535, heads=65, kv=1, ldq=65 * 32, ldo=65 * 32), SHAPE), (lambda: paged(batch=65535, heads=1, kv=1, max_len=33000), SHAPE), (lambda: evict(batch=65535, kv=17), SHAPE)]
+
 
 @pytest.mark.parametrize("i", range(len(CASES)))
 def test_refused_before_anything_is_launched(i):

@@ -190,6 +190,17 @@ def test_heads_that_share_keys_also_share_tiles(dims, layout):
     c.check(what=f"{layout} ")
 
 
+@pytest.mark.parametrize("batch", [64, 65])
+@pytest.mark.parametrize("lens", ["mixed", "equal"])
+def test_batches_that_are_ranked_and_larger_ones(batch, lens):
+    """Up to 64 items are taken by their numbers of keys, equal ones among them; more in order."""
+    klen = [(b * 37) % 150 - 3 for b in range(batch)] if lens == "mixed" else [90] * batch
+    c = Call(batch, 2, 1, 19, 141, 32, klen=klen, seed=batch, fill=float("nan"))
+    c.fwd()
+    c.bwd()
+    c.check(what=f"{lens} ")
+
+
 def test_heads_too_far_apart_to_share_tiles():
     """Shared key heads whose query heads lie more than 31 bits apart: the workspace that is asked for, without layouts, serves this call too."""
     heads, sq, sk, dh, far = 64, 2, 128, 64, (1 << 23) + 8

@@ -193,6 +193,15 @@ def test_attention(lens, heads, kv, dh, page, fp8):
 
 
 @pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("batch", [64, 70])
+def test_attention_of_many_sequences(batch, fp8):
+    """Up to 64 sequences are taken by their lengths, equal ones among them; more in order."""
+    c = Paged([(b * 29) % 90 - 1 for b in range(batch)], 4, 2, 32, 16, fp8, True, seed=batch)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
 def test_attention_rows_apart_factor_and_bounds(fp8):
     Paged([50, 60], 4, 2, 64, 16, fp8, ldq=4 * 64 + 40, alpha=0.75).run()
     c = Paged([50, 60], 4, 2, 64, 16, fp8, ldq=4 * 64 + 40, alpha=0.75, wide=9)
