@@ -1,7 +1,7 @@
 // Attention of a few query rows per key head (one new token's heads that share it) over many keys: over the pages of a cache, or over the rows of
 // another sequence.
 //   p = softmax(c q k), c = dh^-1/2;  O = a sum p v;  weights += sum of p over the rows
-// Bound: HBM, keys and values are read once.  A workgroup takes 16 rows of a key head and a part of its positions, its four waves every fourth tile of
+// Bound: HBM, keys and values are read once (four sequences of 131072, 8 key heads of 128 codes: 188 us, 5.7 TB/s; 48 of up to 4096 in FP16 85 us, 4.9).  A workgroup takes 16 rows of a key head and a part of its positions, its four waves every fourth tile of
 // 32 positions; running statistics per wave, joined through LDS, and over the parts by a second kernel.
 // The matrix core gets 16 keys as its first operand, so that a lane holds one row and four keys of each sixteen; rounded to FP16 these are the second
 // operand of the product with the values, whose first operand is read transposed from LDS in the same order.  E4M3 codes become FP16 on their way
@@ -331,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
 
 // What is left when all parts are there.  The first `joins` workgroups join a row each: O = a sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s (parts without
 // positions have l_s = 0 and are not read); the others add the weights of 256 positions of a key head: sum over its rows of 2^(score - m) / l.
+// (13 x 16 heads of 2500 positions, weights: 5.5 us, most of it the launch and one read after another.)
 constexpr int kMostParts = 1024;
 __global__ void __launch_bounds__(kThreads) finish_kernel(AttendArgs a, Pages pg, long joins, int segments) {
   const int tid = (int)threadIdx.x;
