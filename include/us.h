@@ -548,8 +548,8 @@ typedef struct {
  * be NULL).  Keys and values that several batch items share have a batch stride of 0 in the forward call; heads and rows of the tensors that a call
  * writes must not overlap (US_ERR_SHAPE).  batch and heads up to 65535, batch * heads * ceil(sq / 128) and batch * kv_heads * ceil(sk / 128) up to 2^22.
  * Scores, statistics and all sums are FP32; p, alpha p and ds are rounded to FP16 for their second product, as us_attention_* rounds P and dA (values beyond
- * FP16's range become infinities).  O is read in the backward pass of more than 128 keys, for
- * sum p dp = dO O / alpha.
+ * FP16's range become infinities).  The backward pass takes sum p dp = dO O / alpha from O, but for
+ * few keys (up to 128, of narrow heads more), whose products it makes twice.
  * Workspace (16-byte aligned, contents undefined on entry and exit): us_attention_cross_workspace_bytes, asked with the device current that runs the calls,
  * serves both.  The forward call can do without (NULL: few queries over many keys are then slower, and are added in another order); the backward call needs it.
  * Calls that may overlap on a GPU need a workspace each.  Outputs must not overlap inputs or one another.

@@ -7,7 +7,7 @@
 // product as they lie; the first operand is the tile in LDS, read transposed in the same order.
 // Two products and an exponential per score forward, three for dQ, four for dK and dV.  2 x 32 by 8 heads of 128, 4096 over 8192: forward 1065 to 1145 us by card (1.0 PFLOP/s) and
 // dQ 1475 to 1600 (1.1), bound by power (1.8 GHz, matrix core busy 58 and 64 %); dK and dV 2290 to 2390 (0.94), bound by latency (2.2 GHz): a wave's gradients fill half of the
-// registers.  16 x 16 heads of 64, 512 over 64 to 1024: 31, 45 and 68, bound by the exponentials (vector ALU busy 70 % forward, matrix core 36 %).
+// registers.  16 x 16 heads of 64, 512 over 64 to 1024: 31, 46 and 68, bound by the exponentials (vector ALU busy 70 % forward, matrix core 36 %).
 #include "us_flash.h"
 
 namespace us {
@@ -295,10 +295,13 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows,
 
 // ---- backward: dQ ---------------------------------------------------------------------------------------------------------
 // Comes first and leaves what dK and dV need of every query row, log2(e) L - log2(a) and D.
-// D from the rounded O is off by 2^-12 |O| / a of dO, which next to dO v of n keys is 2^-12 (sum p^2)^1/2: of few keys as much as dS's own rounding.  Up to kFewKeys
-// keys D is therefore the sum of p dO v itself, from products made twice (2-norm error of dQ, unit normal inputs, 5 to 120 keys: 2.95e-4 to 2.98e-4, two roundings to FP16; of 140 to 400 keys, from O,
-// 3.2e-4 to 3.1e-4).
-constexpr int kFewKeys = 128;
+// D from the rounded O is off by 2^-12 |O| / a of dO, which next to dO v of n keys is 2^-12 (sum p^2)^1/2: of few keys as much as dS's own rounding, and of narrow heads more.
+// Up to kFewKeys keys D is therefore the sum of p dO v itself, from products made twice.  2-norm error of dQ in 1e-4, unit normal keys, of 100 / 140 / 300 / 1000 keys (two
+// roundings to FP16 are 2.93): from O all through, 16 columns - / 3.49 / 3.50 / 3.60, 32: - / 3.31 / 3.32 / 3.18, 64: - / 3.26 / 3.14 / 3.06, 128: - / 3.10 / 3.05 / 2.97; from the
+// products 3.0 to 3.1.  So: all keys that one workgroup has up to 32 columns, 256 up to 64, 128 above (us, 16 x 16 heads, 512 over 64 to 1024 keys: of 32 columns 32 -> 46,
+// of 64 44 -> 46).
+template <int NB>
+constexpr int kFewKeys = NB == 1 ? 1 << 30 : NB == 2 ? 256 : 128;
 // Heads of up to 64 columns: 124 registers a lane, so four waves a SIMD.  Of up to 96: three, with fewer fragments read ahead (us: 4 x 32 heads by 8 of 96, 2048 x 2048 370 ->
 // 339, 59 x 6 by 3, 470 x 547 70 -> 65; where a SIMD has one wave it loses half a microsecond of 10).
 // Where a tile is one block of keys (dh > 128) three of them are on their way at a time (us: 32 heads of 256, ragged batch of 5, 869 x 528: 166 -> 156; 130 x 1030:
@@ -371,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 4 : NB == 3 ? 3 : NB <= 4 
   float2 ld = make_float2(__builtin_inff(), 0.0f);
   const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
   if (on && n > 0) ld.x = __builtin_fmaf(a.lse[RowAt(a, kvh, row_again(row0)).of_all(a, b)], kLog2eF, -__builtin_amdgcn_logf(alpha));
-  if (n > kFewKeys) {
+  if (n > kFewKeys<NB> || (begin < end && end - begin < n)) {
     float dot = 0.0f;
     const RowAt mine(a, kvh, row_again(row0));
     const _Float16* o = (const _Float16*)((const uint8_t*)(a.o.p + b * a.o.batch + mine.head * a.o.head) + (long)mine.q * a.o.row);
