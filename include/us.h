@@ -548,7 +548,8 @@ typedef struct {
  * be NULL).  Keys and values that several batch items share have a batch stride of 0 in the forward call; heads and rows of the tensors that a call
  * writes must not overlap (US_ERR_SHAPE).  batch and heads up to 65535, batch * heads * ceil(sq / 128) and batch * kv_heads * ceil(sk / 128) up to 2^22.
  * Scores, statistics and all sums are FP32; p, alpha p and ds are rounded to FP16 for their second product, as us_attention_* rounds P and dA (values beyond
- * FP16's range become infinities).  The backward pass takes sum p dp = dO O / alpha from O, but for
+ * FP16's range become infinities).  An alpha below n_b / 2048, with which those of the backward pass would leave FP16's normal numbers, is raised to that for the rounding
+ * (to n_b^1/2 if that is less), and the quotient taken off in FP32.  The backward pass takes sum p dp = dO O / alpha from O, whose rounding goes into it, but for
  * few keys (up to 128, of narrow heads more), whose products it makes twice.
  * Workspace (16-byte aligned, contents undefined on entry and exit): us_attention_cross_workspace_bytes, asked with the device current that runs the calls,
  * serves both.  The forward call can do without (NULL: few queries over many keys are then slower, and are added in another order); the backward call needs it.

@@ -1,7 +1,7 @@
 // Attention of sq queries over the first n keys of another sequence, forward and backward, without storing the scores.
 //   forward   p = softmax(c q k), c = dh^-1/2;  O = a sum p v;  L = ln sum exp(c q k)
-//   backward  P = a p = exp(c q k - L + ln a),  D = dO O / a = sum p (dO v),  dS = P (dO v - D)
-//             dQ = c dS K,  dK = b c dS^T Q,  dV = b P^T dO
+//   backward  P = f p = exp(c q k - L + ln f),  D = dO O / a = sum p (dO v),  dS = P (dO v - D)
+//             dQ = a / f c dS K,  dK = a / f b c dS^T Q,  dV = a / f b P^T dO        (f: AttendArgs::inner_factor)
 // The matrix core gets keys (forward, dQ) or queries (dK, dV) as its first operand, so that a lane holds one query (one key) and sixteen of the
 // other side: the softmax statistics are scalars of a lane, and its sixteen results are, rounded to FP16, the second operand of the next
 // product as they lie; the first operand is the tile in LDS, read transposed in the same order.
@@ -46,6 +46,11 @@ __device__ __forceinline__ int lane_again() {
   return t & 63;
 }
 __device__ __forceinline__ int row_again(int row0) { return row0 + (lane_again() & 31); }
+// The number of keys, likewise for what is worked out from it.
+__device__ __forceinline__ int keys_again(int n) {
+  asm volatile("" : "+s"(n));
+  return n;
+}
 // Where the rows of a key head's O or dQ start, and those of dK or dV.  (No reference to the kernel's arguments: those are then no longer scalars.)
 struct RowsOfHeads {
   FastDiv by_sq;
@@ -236,8 +241,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) cross_fwd_kernel(At
     if (on && half == 0) a.stats[split * (a.part_stride / a.dh) + row] = make_float2(m * a.c2, sum);
     return;
   }
-  const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
-  const float f = n > 0 ? alpha / sum : 0.0f;
+  const float f = n > 0 ? a.factor(n) / sum : 0.0f;
   store_rows<NB>(lds, acc, f, row0, RowsOfHeads(a, b, kvh, nrows), a.dh, 0, lane, wave);
   if (a.lse && on && half == 0) a.lse[row] = n > 0 ? __builtin_fmaf(__builtin_amdgcn_logf(sum), kLn2F, m * a.c2 * kLn2F) : -__builtin_inff();
 }
@@ -285,7 +289,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows,
     for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], step);
   const int n = a.keys_of(b);
   const bool any = sum != 0.0f;      // (NaN: some)
-  const float f = any ? (a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n)) / sum : 0.0f;
+  const float f = any ? a.factor(n) / sum : 0.0f;
   if (group == 0 && col < a.dh) {
     const v4h o = {to_half(acc[0] * f), to_half(acc[1] * f), to_half(acc[2] * f), to_half(acc[3] * f)};
     wt_store(reinterpret_cast<v4h*>(a.out + b * a.out_batch + head * a.out_head + (long)q * a.out_row + col), o);
@@ -294,7 +298,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows,
 }
 
 // ---- backward: dQ ---------------------------------------------------------------------------------------------------------
-// Comes first and leaves what dK and dV need of every query row, log2(e) L - log2(a) and D.
+// Comes first and leaves what dK and dV need of every query row, log2(e) L - log2(f) and D.
 // D from the rounded O is off by 2^-12 |O| / a of dO, which next to dO v of n keys is 2^-12 (sum p^2)^1/2: of few keys as much as dS's own rounding, and of narrow heads more.
 // Up to kFewKeys keys D is therefore the sum of p dO v itself, from products made twice.  2-norm error of dQ in 1e-4, unit normal keys, of 100 / 140 / 300 / 1000 keys (two
 // roundings to FP16 are 2.93): from O all through, 16 columns - / 3.49 / 3.50 / 3.60, 32: - / 3.31 / 3.32 / 3.18, 64: - / 3.26 / 3.14 / 3.06, 128: - / 3.10 / 3.05 / 2.97; from the
@@ -372,8 +376,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 4 : NB == 3 ? 3 : NB <= 4 
     }
   };
   float2 ld = make_float2(__builtin_inff(), 0.0f);
-  const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
-  if (on && n > 0) ld.x = __builtin_fmaf(a.lse[RowAt(a, kvh, row_again(row0)).of_all(a, b)], kLog2eF, -__builtin_amdgcn_logf(alpha));
+  if (on && n > 0) ld.x = __builtin_fmaf(a.lse[RowAt(a, kvh, row_again(row0)).of_all(a, b)], kLog2eF, -__builtin_amdgcn_logf(a.inner_factor(n)));
   if (n > kFewKeys<NB> || (begin < end && end - begin < n)) {
     float dot = 0.0f;
     const RowAt mine(a, kvh, row_again(row0));
@@ -387,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 4 : NB == 3 ? 3 : NB <= 4 
         for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)x[e], (float)gf[t][e], dot);
       }
     }
-    if (on) ld.y = halves_sum(dot) / alpha;
+    if (on) ld.y = halves_sum(dot) / a.factor(n);
   } else if (begin < end) {
     float ps = 0.0f, pd = 0.0f;
     for (int key = begin, buffer = 0; key < end; key += BK, buffer = (buffer + 1) % C::STAGES) {
@@ -461,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 2 ? 4 : NB == 3 ? 3 : NB <= 4 
     }
   };
   for_stages<C::STAGES>(begin, end, BK, step);
-  const float c = a.c2 * kLn2F;
+  const float c = a.c2 * kLn2F * a.outer_factor(keys_again(n));
   if (n == 1) {
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[j] = zero16();
@@ -657,7 +660,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 3 ? 2 : 1) cross_dkv_kernel(At
       buffer = after;
     }
   }
-  const float c = a.c2 * kLn2F;
+  const float f = a.outer_factor(keys_again(n)), c = a.c2 * kLn2F * f;
   const int key = NB == 3 ? row_again(row0) : row0 + l32;      // (three blocks have not one register to spare)
 #pragma unroll
   for (int j = 0; j < ACC; ++j) {
@@ -671,12 +674,12 @@ __global__ void __launch_bounds__(kThreads, NB <= 3 ? 2 : 1) cross_dkv_kernel(At
 #pragma unroll
     for (int j = 0; j < ACC; ++j) {
       store_block_f32(out, 32 * (first + j), a.dh, on, half_again, dk[j], c);
-      store_block_f32(out + a.dh, 32 * (first + j), a.dh, on, half_again, dv[j], 1.0f);
+      store_block_f32(out + a.dh, 32 * (first + j), a.dh, on, half_again, dv[j], f);
     }
     return;
   }
   store_rows<ACC>(lds, dk, c * a.beta, row0, dk_rows, a.dh, 32 * first, lane_again(), wave);
-  store_rows<ACC>(lds, dv, a.beta, row0, dv_rows, a.dh, 32 * first, lane_again(), wave);
+  store_rows<ACC>(lds, dv, a.beta * f, row0, dv_rows, a.dh, 32 * first, lane_again(), wave);
 }
 
 // Sums of split gradients, part after part: `rows` rows of dh columns `row_stride` elements apart in a part; row = (batch * heads + head) * s + t.

@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
 #pragma unroll
   for (int j = 0; j < 2 * NB; ++j) *reinterpret_cast<v4f*>(mine + 16 * j + 4 * l4) = acc[j];
   __syncthreads();
-  const float alpha = a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)n);
+  const float alpha = a.factor(n);
   const bool parts = a.splits > 1;
   for (int i = (int)threadIdx.x; i < 16 * 8 * NB; i += kThreads) {
     const int r = i / (8 * NB), col = i % (8 * NB) * 4, row = rb * 16 + r;
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(AttendArgs a, Pages pg
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] += x[e];
       }
-      const float f = any ? (a.alpha > 0.0f ? a.alpha : __builtin_sqrtf((float)a.keys_of(b))) / sum : 0.0f;
+      const float f = any ? a.factor(a.keys_of(b)) / sum : 0.0f;
       const v4h h = {to_half(o[0] * f), to_half(o[1] * f), to_half(o[2] * f), to_half(o[3] * f)};
       wt_store(reinterpret_cast<v4h*>(a.out + b * a.out_batch + head * a.out_head + (long)q * a.out_row + col), h);
     }
