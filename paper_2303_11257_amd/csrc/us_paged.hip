@@ -321,9 +321,10 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
         if (page < 0 || page >= pg.pages) continue;
         float* const to = pg.weights + (((long)page * a.kv + kvh) << pg.shift) + (at & ((1 << pg.shift) - 1));
         const float* s = pg.scores + ((long)b * a.heads + kvh * a.rep) * pg.score_ld + at;
-        float w = *to;
+        // (the rows first and in finish_kernel's order: one rounding at the size of what has been added up so far, and the same bits whichever of the two adds)
+        float w = 0.0f;
         for (int r = 0; r < nrows; ++r) w = __builtin_fmaf(__builtin_amdgcn_exp2f(s[r * pg.score_ld] - ms[r]), inv[r], w);
-        *to = w;
+        *to += w;
       }
     }
   }
