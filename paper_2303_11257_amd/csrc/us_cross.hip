@@ -796,7 +796,8 @@ Cut dkv_cut(const CrossCall& c) {
 }
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-size_t rows_bytes(const CrossCall& c) { return up256((size_t)c.batch * c.heads * ((c.sq + 31) / 32 * 32) * 16); }
+// What dQ's kernel leaves of every query row for dK and dV, one row after the other; the parts behind it start on whole 4 KB.
+size_t rows_bytes(const CrossCall& c) { return ((size_t)c.batch * c.heads * c.sq * 16 + 4095) / 4096 * 4096; }
 
 template <class K>
 hipError_t launch(K kernel, FuncConfig& config, int lds, const AttendArgs& a, hipStream_t st) {
