@@ -73,9 +73,9 @@ struct TileReads {
 // 16 bytes per lane straight to LDS, lane after lane from `lds` on; zeros where the offset lies beyond the resource (its four words: buffer_words).  In assembly,
 // because the compiler makes transposing reads of LDS wait for every such load that it knows of, the next tile's too: the kernels wait for what they need themselves
 // (tile_landed, wait_newest).  The compiler's own waits count fewer loads than there are, and so wait longer, never shorter.  (s_nop: five wait states between a
-// vector instruction that writes a scalar register and this load's reading it, one between m0 and the load.)
+// vector instruction that writes a scalar register and this load's reading it, one between m0 and the load.  m0 is an operand, so that the compiler knows what it holds.)
 __device__ __forceinline__ void load_to_lds(v4i from, uint8_t* lds, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)US_LDS_AT(uint8_t, lds)), "v"(off), "s"(from) : "memory");
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"((uint32_t)(uintptr_t)US_LDS_AT(uint8_t, lds)), "v"(off), "s"(from) : "memory");
 }
 // All loads of the workgroup to LDS but each wave's newest N have landed, all its reads of LDS are done; nothing that reads or writes memory moves across.
 template <int N = 0>
