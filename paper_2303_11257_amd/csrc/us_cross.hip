@@ -300,10 +300,12 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttendArgs a, long rows,
 // ---- backward: dQ ---------------------------------------------------------------------------------------------------------
 // Comes first and leaves what dK and dV need of every query row, log2(e) L - log2(f) and D.
 // D from the rounded O is off by 2^-12 |O| / a of dO, which next to dO v of n keys is 2^-12 (sum p^2)^1/2: of few keys as much as dS's own rounding, and of narrow heads more.
-// Up to kFewKeys keys D is therefore the sum of p dO v itself, from products made twice.  2-norm error of dQ in 1e-4, unit normal keys, of 100 / 140 / 300 / 1000 keys (two
-// roundings to FP16 are 2.93): from O all through, 16 columns - / 3.49 / 3.50 / 3.60, 32: - / 3.31 / 3.32 / 3.18, 64: - / 3.26 / 3.14 / 3.06, 128: - / 3.10 / 3.05 / 2.97; from the
-// products 3.0 to 3.1.  So: all keys that one workgroup has up to 32 columns, 256 up to 64, 128 above (us, 16 x 16 heads, 512 over 64 to 1024 keys: of 32 columns 32 -> 46,
-// of 64 44 -> 46).
+// Up to kFewKeys keys D is therefore the sum of p dO v itself, from products made twice.  The aim: a 2-norm error of dQ of at most 3.2e-4, a tenth above that of its two roundings
+// to FP16 (2.93e-4), with queries of 1.5 and unit normal keys.  There, in 1e-4, of 100 / 256 / 1024 / 2000 keys: from O 16 columns 3.54 / 3.54 / 3.51 / 3.52, 32: 3.29 / 3.28 / 3.23 / 3.22,
+// 64: 3.21 / 3.14 / 3.09 / 3.09, 96: 3.15 / 3.10 / 3.05 / 3.03, 128: 3.13 / 3.07 / 3.04 / 3.00; from the products 3.10 to 3.24, 3.02 to 3.07, 2.98 to 3.02, 2.96 to 2.98, 2.95 to 2.97.  (Queries of 3, whose
+// rows are peaked: about 5.1, 4.5, 4.1, 4.0 and 4.0 from O, 3.2 to 3.4 and 3.0 to 3.2 from the products.)  So: all keys that one workgroup has up to 32 columns, 256 up to 64 (48: 3.20 there),
+// 128 above.  Keys in parts, where workgroups are few, take O.  dQ of 16 x 16 heads, 512 queries, us from O and from the products: 32 columns, 64 to 1024 keys 33 and 46; 16 columns,
+// 2000 keys 85 and 150; 64 columns, 256 keys 28.5 and 34; 128 columns, 128 keys 43 and 43.
 template <int NB>
 constexpr int kFewKeys = NB == 1 ? 1 << 30 : NB == 2 ? 256 : 128;
 // Heads of up to 64 columns: 124 registers a lane, so four waves a SIMD.  Of up to 96: three, with fewer fragments read ahead (us: 4 x 32 heads by 8 of 96, 2048 x 2048 370 ->
