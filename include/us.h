@@ -589,7 +589,8 @@ size_t us_attention_cross_workspace_bytes(long batch, long heads, long kv_heads,
  *   [batch, table_to_ld], pages of the same pools that hold none of the sequences): the kept rows are copied there.
  *   new_len[b] = min(len[b], keep) (int32 [batch], may be len itself, or NULL), kept: int32 [batch, kv_heads, keep], the positions that were kept, -1 behind a shorter
  *   sequence's.  0 <= recent <= keep <= 2^20.  max_len as above.  A position on a page that there is not comes after all others; where it is kept all the same, no row
- *   moves, and its new slot is left as it was.
+ *   moves, and its new slot is left as it was.  Weights come from the queries of us_attention_paged alone: before a prompt's first new tokens they are what the caller put there, and of
+ *   equal ones the lowest positions stay.
  *
  * dh a multiple of 16 up to US_ROPE_HEAD_MAX; batch and heads up to 65535; batch * heads up to 2^22, batch * kv_heads * ceil(max_len / 256) up to 2^23 (eviction:
  * batch * kv_heads up to 2^20); a sequence's new rows, s * kv_heads * dh / 8, up to 2^31 - 1.  All pools and rows 16-byte aligned.  Results do not depend on scheduling.

@@ -69,7 +69,7 @@ constexpr int kSelect = 1024, kSelectWaves = kSelect / 64;
 // Bound by latency: four rounds, each a pass over LDS bins and two barriers (16 x 8 heads of up to 8192 positions 17.8 us for 4 MB).
 // A workgroup per sequence and key head: the k-th largest weight by four rounds of 256 bins, then the positions above it, and of those equal to it the
 // first ones, in their order.  A wave has a run of neighbouring positions, so that its part of the order needs one exchange of counts with the others;
-// up to PER of them per lane stay in registers (PER = 0: longer sequences read the weights again each round).
+// up to PER of them per lane stay in registers (PER = 0: longer sequences read the weights again each round, page by page: 4 x 8 heads of 131072 positions 378 us for 17 MB).
 template <int PER>
 __global__ void __launch_bounds__(kSelect) cache_select_kernel(Pool p, const float* weights, const int* len, int* kept, int max_len, int keep, int recent) {
   __shared__ uint32_t bins[2][256];

@@ -6,8 +6,9 @@
 // other side: the softmax statistics are scalars of a lane, and its sixteen results are, rounded to FP16, the second operand of the next
 // product as they lie; the first operand is the tile in LDS, read transposed in the same order.
 // Two products and an exponential per score forward, three for dQ, four for dK and dV.  2 x 32 by 8 heads of 128, 4096 over 8192: forward 1065 to 1145 us by card (1.0 PFLOP/s) and
-// dQ 1475 to 1600 (1.1), bound by power (1.8 GHz, matrix core busy 58 and 64 %); dK and dV 2290 to 2390 (0.94), bound by latency (2.2 GHz): a wave's gradients fill half of the
-// registers.  16 x 16 heads of 64, 512 over 64 to 1024: 31, 46 and 68, bound by the exponentials (vector ALU busy 70 % forward, matrix core 36 %).
+// dQ 1475 to 1600 (1.1), bound by power (1.7 GHz, matrix core busy 58 and 64 % of a CU's busy cycles, vector ALU 47 and 39); dK and dV 2230 to 2390 (0.96), bound by latency (49 and
+// 29 %; 1.9 to 2.2 GHz by card): a wave's gradients fill half of the registers.  16 x 16 heads of 64, 512 over 64 to 1024: 31, 46 and 67: matrix core busy 36, 40 and 38 %, vector ALU
+// (which the products' issue is part of) 70, 60 and 37 %, one after the other for the most part, and CUs busy for 63 to 70 % of the time, for the items' lengths differ.
 #include "us_flash.h"
 
 namespace us {

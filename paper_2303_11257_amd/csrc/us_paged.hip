@@ -88,7 +88,8 @@ __global__ void __launch_bounds__(kThreads, NB <= 4 ? 2 : 1) few_rows_kernel(Att
   const uint32_t split = pg.by_groups.of(blockIdx.x);
   const uint32_t i0 = blockIdx.x - split * pg.groups, group = pg.by_tiles.of(i0);
   const int rb = (int)(i0 - group * a.tiles);
-  // (the longest sequences first: 93 us -> 85 there; not where lengths are those of one encoder: 32 x 16 heads over 1500 keys of 64 42.7 us, ranked 44.5)
+  // (the longest sequences first: 93 us -> 85 there; not over another sequence's keys, us in order and ranked: 32 x 16 heads of 64, one query, 1500 keys each 42.7 and 44.5, 47 to 1500
+  // 23.0 and 23.3; 48 x 32 by 8 of 128, 85 to 4096 88.2 and 89.6; 32 x 32 by 8 of 128, 47 to 1500 30.5 and 28.8; 16 x 12 of 64, 32 to 512 11.2 and 12.0)
   const int slot = (int)pg.by_kv.of(group), kvh = (int)(group - (uint32_t)slot * a.kv), b = PAGED ? a.by_keys(slot) : slot;
   const int n = a.keys_of(b);
   const int begin = (int)split * a.per_split, end = begin + a.per_split < n ? begin + a.per_split : n;
@@ -555,6 +556,9 @@ hipError_t launch_paged(const PagedCall& c, void* workspace, hipStream_t st) {
   return finish(a, pg, c.weights && a.stats ? c.max_len : 0, st);
 }
 
+// Up to one tile of rows.  us of this kernel, and of the forward kernel of many queries (us_cross.hip): 32 x 16 heads of 64 over 1500 keys, 1 / 16 rows 37.6 / 38.2, 48.4 / 42.8;
+// 2 x 32 by 8 of 128 over 8192, 16 rows 21.4, 20.7; one of 8 heads of 64 over 20000, 8 rows 13.1, 13.1; 16 x 16 of 64 over 512, 1 / 16 rows 14.3 / 18.1, 11.5 / 11.3; 4 x 8 of 256
+// over 1500, 1 / 16 rows 23.0 / 28.3, 21.9 / 22.1.  Two tiles, 32 rows: 58 and 43, 30.0 and 21.0, 14.0 and 13.8, 14.0 and 11.5, 42 and 23.
 bool few_rows_take(long heads, long kv_heads, long sq) { return sq * (heads / kv_heads) <= 16; }
 size_t few_rows_workspace_bytes(long batch, long heads, long kv, long sq, long sk, long dh) {
   const Room r = room(batch, heads, kv, heads / kv * sq, sq, dh, sk, false);
